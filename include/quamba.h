@@ -570,6 +570,54 @@ int quamba_model_generate(const quamba_model *model, const int32_t *first_tokens
                           quamba_half *conv_states, void *ws, size_t ws_bytes, int use_graph,
                           void *stream);
 
+/* ---- Layers kept in 16 bits (hybrid stacks: not every layer of a model is a quantized Mamba block).  Operands are fp16 or
+ * bf16, results of that type or fp32, sums and states fp32.  Rows may be parts of wider rows: every stride is given in
+ * elements, so q, k and v can be columns of one projection's output.  Buffers need no more than their elements' alignment;
+ * where rows start on 16 bytes (pointers and strides) the loads are wider and the calls faster.
+ *
+ * quamba_linear: the projection  out[m, :] = act(x[m, :] W^T + bias) + residual[m, :]
+ *   x [M, K] row stride ldx, W [N, K] row stride ldw, both of `type` (QUAMBA_TYPE_F16 / QUAMBA_TYPE_BF16); bias fp32 [N] or NULL;
+ *   residual [M, N] row stride ldr, of the output's type, or NULL; out [M, N] row stride ldo, `type` or QUAMBA_TYPE_F32.
+ *   act: QUAMBA_ACT_*; GELU = v Phi(v), GELU_TANH its tanh form, SILU = v sigmoid(v).  Sums, bias, activation and residual are
+ *   fp32, rounded once to the output.  residual may be `out` itself (ldr = ldo), the residual stream updated in place; otherwise
+ *   out must not overlap any input.  A row's result is the same whatever other rows hold, but may differ in the last bits
+ *   between calls of different M (another order of the sums).
+ *   ws (16-byte aligned, may be NULL): room for the partial sums of a K split over the grid; with less than
+ *   quamba_linear_workspace_bytes K is split less or not at all, which only costs time.  M = 0 is allowed and does nothing. */
+#define QUAMBA_TYPE_F16 1
+#define QUAMBA_TYPE_BF16 2
+#define QUAMBA_TYPE_F32 3
+#define QUAMBA_ACT_NONE 0
+#define QUAMBA_ACT_RELU 1
+#define QUAMBA_ACT_SILU 2
+#define QUAMBA_ACT_GELU 3
+#define QUAMBA_ACT_GELU_TANH 4
+#define QUAMBA_ACT_SIGMOID 5
+size_t quamba_linear_workspace_bytes(int M, int N, int K);
+int quamba_linear(int type, const void *x, int ldx, const void *W, int ldw, const float *bias, const void *residual, int ldr,
+                  int M, int N, int K, int act, int out_type, void *out, int ldo, void *ws, size_t ws_bytes, void *stream);
+
+/* Linear attention with a decay for each head, the recurrence with a matrix for a state:
+ *   S_t = a_t S_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t,   a_t = exp(min(g_t, 0))
+ *   q, k [Bt, L, Hk, dk] and v [Bt, L, Hv, dv] of `type`: token t of sequence b starts at (b L + t) * ldq (ldk, ldv) elements,
+ *   its heads follow one another; value head h reads key head h / (Hv / Hk) (Hv a multiple of Hk).  dk <= 256, dv <= 1024.
+ *   log_decay g fp32 [Bt, L, Hv], token stride ldg; ldg = 0: one decay per head, [Hv]; NULL: no decay.  A positive g counts as 0;
+ *   g = -infinity (or so low that exp(g) leaves fp32's normal range) forgets everything before its token exactly.
+ *   out [Bt, L, Hv, dv] of `type`, token stride ldo.  state [Bt, Hv, dk, dv] fp32, dense, 16-byte aligned, in/out; prompts may
+ *   pass NULL (start from zero, keep nothing).
+ * quamba_linattn_prefill runs prompts: lens int32 [Bt] (device, may be NULL = L each) gives each sequence's length, clamped to
+ * [0, L]; tokens behind it are not read, their output rows are left as they were, and an empty sequence keeps its state.  The sums are
+ * taken block by block: the result is that of the recurrence up to the rounding of fp32 sums (block weights carry 16 bits or more,
+ * the state's update 22 or more).  Workspace: quamba_linattn_workspace_bytes, 256-byte aligned.
+ * quamba_linattn_step is one token of every sequence (L = 1, state required), strides between sequences.
+ * out must not overlap an input, state no other buffer.  Bt = 0 or L = 0 does nothing. */
+size_t quamba_linattn_workspace_bytes(int Bt, int L, int Hk, int Hv, int dk, int dv);
+int quamba_linattn_prefill(int type, const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, const float *log_decay,
+                           int ldg, const int32_t *lens, int Bt, int L, int Hk, int Hv, int dk, int dv, float scale, void *out, int ldo,
+                           float *state, void *ws, size_t ws_bytes, void *stream);
+int quamba_linattn_step(int type, const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, const float *log_decay,
+                        int ldg, int Bt, int Hk, int Hv, int dk, int dv, float scale, void *out, int ldo, float *state, void *stream);
+
 /* ---------------------------------------------------------------------------------------
  * Diagnostics: instruction-rate probes behind the roofline statements (no part of the method).
  * A probe is one kernel of register-only loops on every SIMD of the chip (256 CUs x 4 SIMDs x

@@ -39,3 +39,4 @@ from .x_asym import calibrate_xasym, q_prefill_xasym, q_decode_xasym, quantize_a
 from .x_formats import (calibrate_xfmt, q_prefill_xfmt, q_decode_xfmt, encode_e4m3, decode_e4m3,  # noqa: F401
                         encode_log2, decode_log2)
 from .x_dynamic import q_prefill_xdyn, q_decode_xdyn, dynamic_scale, dynamic_multipliers  # noqa: F401
+from .layers16 import activate, linear, linattn  # noqa: F401

@@ -27,6 +27,8 @@ __all__ = [
     "XFmt", "XFMT_FIELDS", "XFMT_E4M3", "XFMT_LOG2", "make_xfmt", "xfmt_to_dict", "quamba_calibrate_xfmt",
     "quamba_mixer_prefill_xfmt", "quamba_mixer_decode_xfmt", "quamba_x_encode", "quamba_xfmt_proj",
     "quamba_xdyn_workspace_bytes", "quamba_mixer_prefill_xdyn", "quamba_mixer_decode_xdyn",
+    "TYPE_F16", "TYPE_BF16", "TYPE_F32", "ACT_NONE", "ACT_RELU", "ACT_SILU", "ACT_GELU", "ACT_GELU_TANH", "ACT_SIGMOID",
+    "quamba_linear_workspace_bytes", "quamba_linear", "quamba_linattn_workspace_bytes", "quamba_linattn_prefill", "quamba_linattn_step",
     "quamba_debug_set_gemm_variant", "quamba_debug_set_gemm_split", "quamba_debug_set_gemv_max_rows",
     "quamba_debug_set_fuse_dt", "quamba_debug_set_fuse_decode", "quamba_debug_set_scan_variant",
     "quamba_debug_set_decode_stack", "quamba_debug_gemm_kind", "quamba_debug_xfmt_column_tiles", "quamba_debug_last_block_reads_ahead",
@@ -38,6 +40,8 @@ __all__ = [
 ]
 
 X_PERCENTILE, X_MSE_CLIP = 0, 1
+TYPE_F16, TYPE_BF16, TYPE_F32 = 1, 2, 3
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH, ACT_SIGMOID = 0, 1, 2, 3, 4, 5
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -340,6 +344,15 @@ def lib():
     L.quamba_mixer_prefill_xdyn.argtypes = [P(Dims), P(QWeights), P(Scales), vp, i, i, vp, vp, vp, P(Taps), vp, vp, vp, sz, vp]
     L.quamba_mixer_decode_xdyn.argtypes = [P(Dims), P(QWeights), P(Scales), vp, i, vp, vp, vp, P(Taps), vp, vp, vp, sz, vp]
     for name in ("quamba_mixer_prefill_xdyn", "quamba_mixer_decode_xdyn"):
+        getattr(L, name).restype = C.c_int
+    L.quamba_linear_workspace_bytes.restype = sz
+    L.quamba_linear_workspace_bytes.argtypes = [i, i, i]
+    L.quamba_linear.argtypes = [i, vp, i, vp, i, vp, vp, i, i, i, i, i, i, vp, i, vp, sz, vp]
+    L.quamba_linattn_workspace_bytes.restype = sz
+    L.quamba_linattn_workspace_bytes.argtypes = [i, i, i, i, i, i]
+    L.quamba_linattn_prefill.argtypes = [i, vp, i, vp, i, vp, i, vp, i, vp, i, i, i, i, i, i, f, vp, i, vp, vp, sz, vp]
+    L.quamba_linattn_step.argtypes = [i, vp, i, vp, i, vp, i, vp, i, i, i, i, i, i, f, vp, i, vp, vp]
+    for name in ("quamba_linear", "quamba_linattn_prefill", "quamba_linattn_step"):
         getattr(L, name).restype = C.c_int
     L.quamba_mixer_fp32.argtypes = [P(Dims), P(FpWeights), vp, i, i, vp, vp, sz, vp]
     for name in ("quamba_calibrate_x_rule", "quamba_clip_search", "quamba_mixer_fp32"):
@@ -695,6 +708,35 @@ def quamba_calibrate_block(dims, fp_weights, norm_w, eps, res, out, nb, Lc, x_pe
                                         nb, Lc, float(x_percentile), C.byref(oq), C.byref(sc), _ptr(ws), _nbytes(ws),
                                         _stream(stream)))
     return sc
+
+
+# ---- layers kept in 16 bits; `type` is TYPE_F16 / TYPE_BF16, strides count elements
+def quamba_linear_workspace_bytes(M, N, K) -> int:
+    return int(lib().quamba_linear_workspace_bytes(M, N, K))
+
+
+def quamba_linear(type, x, ldx, W, ldw, bias, residual, ldr, M, N, K, act, out_type, out, ldo, ws, stream=None):
+    """out = act(x W^T + bias) + residual; `bias`, `residual` and `ws` may be None."""
+    _check(lib().quamba_linear(type, _ptr(x), ldx, _ptr(W), ldw, _ptr(bias), _ptr(residual), ldr, M, N, K, act, out_type,
+                               _ptr(out), ldo, _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def quamba_linattn_workspace_bytes(Bt, L, Hk, Hv, dk, dv) -> int:
+    return int(lib().quamba_linattn_workspace_bytes(Bt, L, Hk, Hv, dk, dv))
+
+
+def quamba_linattn_prefill(type, q, ldq, k, ldk, v, ldv, log_decay, ldg, lens, Bt, L, Hk, Hv, dk, dv, scale, out, ldo, state, ws,
+                           stream=None):
+    """Prompts; `log_decay`, `lens` and `state` may be None."""
+    _check(lib().quamba_linattn_prefill(type, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(log_decay), ldg, _ptr(lens), Bt, L, Hk,
+                                        Hv, dk, dv, float(scale), _ptr(out), ldo, _ptr(state), _ptr(ws), _nbytes(ws),
+                                        _stream(stream)))
+
+
+def quamba_linattn_step(type, q, ldq, k, ldk, v, ldv, log_decay, ldg, Bt, Hk, Hv, dk, dv, scale, out, ldo, state, stream=None):
+    """One token of every sequence; `state` is updated in place."""
+    _check(lib().quamba_linattn_step(type, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(log_decay), ldg, Bt, Hk, Hv, dk, dv,
+                                     float(scale), _ptr(out), ldo, _ptr(state), _stream(stream)))
 
 
 # ---- tuning hooks (process-wide switches between kernels that compute the same thing)
