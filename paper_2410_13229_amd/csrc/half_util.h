@@ -39,4 +39,17 @@ __device__ __forceinline__ T from_f32(float v) {
   return static_cast<T>(v);
 }
 
+// Eight consecutive elements of a row from element k on, zeros past K.  A 16-byte load at any element's address.
+template <typename T>
+__device__ __forceinline__ typename Half<T>::v8 row8(const T *row, int k, int K) {
+  typename Half<T>::v8 v;
+  if (k + 8 <= K) {
+    __builtin_memcpy(&v, row + k, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = k + e < K ? row[k + e] : static_cast<T>(0.f);
+  }
+  return v;
+}
+
 }  // namespace quamba

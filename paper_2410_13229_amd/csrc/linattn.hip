@@ -1,6 +1,7 @@
 // Linear attention with a decay per head:  S_t = a_t S_{t-1} + k_t v_t^T,  o_t = scale q_t^T S_t,  a_t = exp(min(g_t, 0)),
 // S [dk, dv] in fp32 per sequence and value head.
 #include <climits>
+#include <type_traits>
 
 #include "common.h"
 #include "half_util.h"
@@ -67,6 +68,559 @@ __global__ __launch_bounds__(256) void linattn_tokens_kernel(LinAttnArgs a) {
       if (r0 + i < a.dk && col < a.dv) st[(size_t)(r0 + i) * a.dv + col] = S[i];
 }
 
+// ------------------------------------------------------------------------------------------------------------------
+// Prompts, in blocks of 64 tokens.  With G_t the sum of the block's log2 decays up to token t,
+//   o_t = scale (exp2(G_t) q_t^T S + sum_{s <= t} exp2(G_t - G_s) (q_t . k_s) v_s),   S <- exp2(G_64) S + sum_s k_s (exp2(G_64 - G_s) v_s)^T
+// four products per block, all on the matrix units; no exponential has a positive argument.
+//
+// A workgroup of four waves takes 64 NT columns of one value head's state and walks a range of blocks; a wave keeps its 16 NT
+// columns of S (all rows) in fp32 registers.  Result registers of a 16 x 16 product hold 4 rows of one column, operand
+// registers 8 rows of one column, and which 8 of 32 rows a group of 16 lanes contributes is free as long as both operands
+// agree: taking rows 16 a + 4 g + r turns S's result registers into operands of the next product without moving them.
+//
+// fp32 values go through the 16-bit matrix units in pieces, each the rounding of what the ones before left over:
+//   S in front of q: two pieces (16 bits), the block's weights two bf16 pieces, the weighted v of the state's update three bf16
+//   pieces (24 bits) or two fp16 ones (22).  bf16 pieces have fp32's range.  fp16 operands (k, q) need fp16 partners, so a
+//   column of S or of the weighted v is first brought to the top of fp16's range by a power of two; v itself splits into two
+//   bf16 pieces exactly.
+// A decay of -infinity (or below fp32's range) is a reset: it adds nothing to G but starts a new stretch, and weights between
+// different stretches are 0.
+// ------------------------------------------------------------------------------------------------------------------
+constexpr int kBlock = 64;
+
+struct SegArgs {
+  int segments, blocks;  // of a sequence; blocks of a segment
+  int pair0, pairs;      // (sequence, value head) pairs b Hv + h of this launch
+  float *slots;          // [pairs][segments][dk][dv]: a segment's own sum of updates at slot + 1, later the state it starts from
+  float2 *decays;        // [pairs][segments]: a segment's whole decay, fp32 and what that rounding left over
+};
+
+struct GTable {  // of a block's 64 tokens
+  float d[kBlock];     // log2 decays summed from the token's group of 16 on
+  int n[kBlock];       // stretch (resets up to the token)
+  float e[kBlock];     // exp2(G_t), 0 behind a reset
+  float w[kBlock];     // exp2(G_64 - G_s), 0 in front of a reset
+  float between[16];   // 4 tb + sb: sums in front of group tb less those in front of group sb
+  float dec, dec_lo;   // exp2(G_64)
+  int resets;
+  double sum;          // G_64
+};
+
+// 2^x for x <= 0, to 7e-12: a state's decays multiply up over its blocks, so fp32's rounding of one would show after a hundred
+__device__ __forceinline__ double exp2_neg(double x) {
+  if (!(x > -200.0)) return x == x ? 0.0 : x;
+  const double n = __builtin_rint(x), f = (x - n) * 0.69314718055994530942;
+  double p = 1.0 / 362880.0;
+  p = __builtin_fma(p, f, 1.0 / 40320.0);
+  p = __builtin_fma(p, f, 1.0 / 5040.0);
+  p = __builtin_fma(p, f, 1.0 / 720.0);
+  p = __builtin_fma(p, f, 1.0 / 120.0);
+  p = __builtin_fma(p, f, 1.0 / 24.0);
+  p = __builtin_fma(p, f, 1.0 / 6.0);
+  p = __builtin_fma(p, f, 0.5);
+  p = __builtin_fma(p, f, 1.0);
+  p = __builtin_fma(p, f, 1.0);
+  return __builtin_ldexp(p, (int)n);
+}
+
+// A double moved by a DPP pattern, 0 where no lane supplies it.
+template <int CTRL>
+__device__ __forceinline__ double dpp_f64(double v) {
+  const long long b = __double_as_longlong(v);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, 0xf, 0xf, true);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, 0xf, 0xf, true);
+  return __longlong_as_double(((long long)hi << 32) | (unsigned)lo);
+}
+__device__ __forceinline__ double lane_f64(double v, int lane) {
+  const long long b = __double_as_longlong(v);
+  return __longlong_as_double(((long long)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32) |
+                              (unsigned)__builtin_amdgcn_readlane((int)b, lane));
+}
+
+// One wave, lane = token: the table of a block from the tokens' log decays (0 behind the end).
+__device__ __forceinline__ void make_table(float g, int lane, GTable &t) {
+  const bool reset = g < -87.f;  // exp leaves fp32's normal range: nothing of the past remains
+  const double x = reset || g > 0.f ? 0.0 : (double)g * 1.44269504088896340736;
+  double d = x;  // inclusive sums inside rows of 16 lanes
+  d += dpp_f64<0x111>(d);  // row_shr 1
+  d += dpp_f64<0x112>(d);
+  d += dpp_f64<0x114>(d);
+  d += dpp_f64<0x118>(d);
+  const double b1 = lane_f64(d, 15), b2 = b1 + lane_f64(d, 31), b3 = b2 + lane_f64(d, 47), all = b3 + lane_f64(d, 63);
+  const double G = d + (lane < 16 ? 0.0 : (lane < 32 ? b1 : (lane < 48 ? b2 : b3)));
+  const unsigned long long m = __ballot(reset);
+  const int n = __popcll(m & (~0ull >> (63 - lane))), last = __popcll(m);
+  t.d[lane] = (float)d;
+  t.n[lane] = n;
+  t.e[lane] = n ? 0.f : __builtin_amdgcn_exp2f((float)G);
+  t.w[lane] = n != last ? 0.f : __builtin_amdgcn_exp2f((float)(all - G));
+  const double dec = last ? 0.0 : exp2_neg(all);
+  const int tb = lane >> 2, sb = lane & 3;
+  const double bt = tb == 0 ? 0.0 : (tb == 1 ? b1 : (tb == 2 ? b2 : b3)), bs = sb == 0 ? 0.0 : (sb == 1 ? b1 : (sb == 2 ? b2 : b3));
+  if (lane < 16) t.between[lane] = (float)(bt - bs);
+  if (lane == 0) {
+    t.dec = (float)dec;
+    t.dec_lo = (float)(dec - (double)(float)dec);
+    t.resets = last;
+    t.sum = all;
+  }
+}
+
+// LDS rows of 32 KT elements whose 16-byte chunks are exchanged so that 16 rows at one chunk, and 8 rows (0-7 or 8-15) at two
+// adjacent chunks (the transposing reads), fall on different banks.
+template <int KT>
+__device__ __forceinline__ int tile_at(int row, int chunk) {
+  const int f = KT == 2 ? (((row >> 1) & 3) << 1) | ((row >> 3) & 1) : ((row & 7) << 1) | ((row >> 3) & 1);
+  return row * (64 * KT) + ((chunk ^ f) << 4);
+}
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+// Four elements of column `lane % 16` of a 16-column block: rows row0 .. row0 + 3, row0 = 4 (lane / 16) + first.  Each lane
+// points at 4 elements of one row; the read exchanges them inside groups of 16 lanes.
+template <typename T, int KT>
+__device__ __forceinline__ typename Half<T>::v4 read_columns(const char *tile, int first, int block, int lane) {
+  const int i = lane & 15, row = first + 4 * (lane >> 4) + (i >> 2), chunk = 2 * block + ((i & 3) >> 1);
+  const char *p = tile + tile_at<KT>(row, chunk) + (i & 1) * 8;
+  const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3))) *)(p));
+  return __builtin_bit_cast(typename Half<T>::v4, r);
+}
+// Operand of 32 rows (tokens) of a column block: rows 32 kb + 16 a + 4 g + r in slot 4 a + r of lane group g
+template <typename T, int KT>
+__device__ __forceinline__ typename Half<T>::v8 column_operand(const char *tile, int kb, int block, int lane) {
+  const auto lo = read_columns<T, KT>(tile, 32 * kb, block, lane), hi = read_columns<T, KT>(tile, 32 * kb + 16, block, lane);
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// Operand of one row: elements 32 j + 16 a + 4 g + r in slot 4 a + r
+template <typename T, int KT>
+__device__ __forceinline__ typename Half<T>::v8 row_operand(const char *tile, int row, int j, int lane) {
+  const int g = lane >> 4, chunk = 4 * j + (g >> 1), off = (g & 1) * 8;
+  const auto lo = *reinterpret_cast<const typename Half<T>::v4 *>(tile + tile_at<KT>(row, chunk) + off);
+  const auto hi = *reinterpret_cast<const typename Half<T>::v4 *>(tile + tile_at<KT>(row, chunk + 2) + off);
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// 2^-(exponent of m) brought to the top of fp16's range (2^12 .. 2^13), its exponent limited so that it stays an ordinary fp32
+// number; m = 0 and m = infinity or NaN too
+__device__ __forceinline__ int top_exponent(float m) {
+  const int e = 127 + 12 - (int)((__float_as_uint(m) >> 23) & 0xff);
+  return min(max(e, -100), 100);
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(127 + e) << 23); }
+// Largest over the four lane groups (the same column)
+__device__ __forceinline__ float max_over_groups(float m) {
+  m = fmaxf(m, __shfl_xor(m, 16));
+  return fmaxf(m, __shfl_xor(m, 32));
+}
+
+__device__ __forceinline__ int seq_len(const LinAttnArgs &a, int b) { return a.lens ? min(max(a.lens[b], 0), a.L) : a.L; }
+
+// KT: dk <= 32 KT.  OUT: outputs and the state; otherwise only a segment's own sum of updates and its decay.
+template <typename T, int KT, int NT, bool OUT>
+__global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, SegArgs sg) {
+  constexpr bool F16 = std::is_same<T, _Float16>::value;
+  constexpr int VT = 2 * NT;                                  // 32-element blocks of a row of v: 64 NT columns
+  constexpr int QB = OUT ? 64 * KT * kBlock : 0, KB = 64 * KT * kBlock, VB = 64 * VT * kBlock, PB = OUT ? 128 * kBlock : 0;
+  typedef typename Half<T>::v8 v8;
+  typedef Half<__bf16>::v8 b8;
+  typedef Half<__bf16>::v4 b4;
+  __shared__ __attribute__((aligned(16))) char lds[QB + KB + VB + 2 * PB];
+  __shared__ GTable tables[2];
+  char *lq = lds, *lk = lds + QB, *lv = lk + KB, *lp = lv + VB, *lpl = lp + PB;
+
+  // XCDs get contiguous runs of workgroups (ids are dealt round-robin to the 8 of them): column parts of a head, heads of a
+  // segment next to one another, so what shares q and k shares an L2
+  const int nwg = gridDim.x, per = nwg >> 3;
+  const int id = (int)blockIdx.x < (per << 3) ? ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
+  const int parts = (a.dv + 64 * NT - 1) / (64 * NT);
+  const int part = id % parts, rest = id / parts;
+  const int slot = rest % sg.pairs, seg = rest / sg.pairs, pair = sg.pair0 + slot;
+  const int h = pair % a.Hv, b = pair / a.Hv, hk = h / (a.Hv / a.Hk);
+  const int len = seq_len(a, b);
+  const int t_lo = seg * sg.blocks * kBlock, t_hi = min(len, t_lo + sg.blocks * kBlock);
+  if (t_lo >= len || (!OUT && t_hi == len)) return;  // nothing here; the last segment's sum is nobody's start
+
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col0 = part * 64 * NT + wave * 16 * NT;  // this wave's first column
+
+  const size_t row0 = (size_t)b * a.L;
+  const T *pq = static_cast<const T *>(a.q) + row0 * a.ldq + (size_t)hk * a.dk;
+  const T *pk = static_cast<const T *>(a.k) + row0 * a.ldk + (size_t)hk * a.dk;
+  const T *pv = static_cast<const T *>(a.v) + row0 * a.ldv + (size_t)h * a.dv + part * 64 * NT;
+  const int dv_part = a.dv - part * 64 * NT;
+  T *po = static_cast<T *>(a.out) + row0 * a.ldo + (size_t)h * a.dv;
+
+  // a block's rows, 16 bytes a lane along them: zeros behind the end and behind dk or dv
+  constexpr int CPK = 4 * KT, CPV = 4 * VT, NK = kBlock * CPK / 256, NV = kBlock * CPV / 256;
+  v8 rq[OUT ? NK : 1], rk[NK], rv[NV];
+  const v8 zero = {};
+  float gt = 0.f;
+  auto fetch = [&](int t0) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int ch = tid + 256 * i, t = t0 + ch / CPK, e = ch % CPK * 8;
+      if constexpr (OUT) rq[i] = t < t_hi ? row8(pq + (size_t)t * a.ldq, e, a.dk) : zero;
+      rk[i] = t < t_hi ? row8(pk + (size_t)t * a.ldk, e, a.dk) : zero;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int ch = tid + 256 * i, t = t0 + ch / CPV, e = ch % CPV * 8;
+      rv[i] = t < t_hi ? row8(pv + (size_t)t * a.ldv, e, dv_part) : zero;
+    }
+    gt = 0.f;
+    const int t = t0 + lane;
+    if (a.g && t < t_hi) gt = a.ldg ? a.g[(row0 + t) * a.ldg + h] : a.g[h];
+  };
+  auto park = [&]() {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int ch = tid + 256 * i;
+      if constexpr (OUT) *reinterpret_cast<v8 *>(lq + tile_at<KT>(ch / CPK, ch % CPK)) = rq[i];
+      *reinterpret_cast<v8 *>(lk + tile_at<KT>(ch / CPK, ch % CPK)) = rk[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int ch = tid + 256 * i;
+      *reinterpret_cast<v8 *>(lv + tile_at<VT>(ch / CPV, ch % CPV)) = rv[i];
+    }
+  };
+
+  fetch(t_lo);
+
+  // S[m][n]: rows 16 m + 4 g + r of column col0 + 16 n + c
+  v4f S[2 * KT][NT];
+  const float *from = !OUT ? nullptr : (sg.segments > 1 ? sg.slots + ((size_t)slot * sg.segments + seg) * a.dk * a.dv
+                                                        : (a.state ? a.state + (size_t)pair * a.dk * a.dv : nullptr));
+#pragma unroll
+  for (int m = 0; m < 2 * KT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * m + 4 * g + r, col = col0 + 16 * n + c;
+        S[m][n][r] = from && row < a.dk && col < a.dv ? from[(size_t)row * a.dv + col] : 0.f;
+      }
+
+  if constexpr (OUT) {
+    // the blocks of weights above the diagonal that a product of 32 tokens takes in: zero, and never written again
+    for (int i = tid; i < 2 * 2 * 16 * 2; i += 256) {  // piece, block pair, row, chunk
+      const int piece = i & 1, pr = (i >> 1) & 1, row = 32 * pr + ((i >> 2) & 15), chunk = 4 * pr + 2 + (i >> 6);
+      *reinterpret_cast<b8 *>((piece ? lpl : lp) + tile_at<2>(row, chunk)) = b8{};
+    }
+  }
+  double G = 0.0;  // of the segment
+  int resets = 0;
+  if (wave == 0) make_table(gt, lane, tables[0]);
+  park();
+  __syncthreads();
+
+  int buf = 0;
+  for (int t0 = t_lo; t0 < t_hi; t0 += kBlock, buf ^= 1) {
+    const GTable &tab = tables[buf];
+    const bool more = t0 + kBlock < t_hi;
+    if (more) fetch(t0 + kBlock);
+
+    v4f O[4][NT];  // transposed: columns (of v) 4 g + r, token 16 tb + c
+    if constexpr (OUT) {
+      // weights: 10 blocks of 16 x 16 on and below the diagonal, dealt to the waves
+      for (int id10 = wave; id10 < 10; id10 += 4) {
+        const int tb = id10 < 1 ? 0 : (id10 < 3 ? 1 : (id10 < 6 ? 2 : 3)), sb = id10 - tb * (tb + 1) / 2;
+        v4f p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < KT; ++j) {
+          const v8 fk = *reinterpret_cast<const v8 *>(lk + tile_at<KT>(16 * sb + c, 4 * j + g));
+          const v8 fq = *reinterpret_cast<const v8 *>(lq + tile_at<KT>(16 * tb + c, 4 * j + g));
+          p = Half<T>::mfma16(fk, fq, p);  // rows s, columns t
+        }
+        const int t = 16 * tb + c, s = 16 * sb + 4 * g;
+        const float dt = tab.d[t] + tab.between[4 * tb + sb];
+        const int nt = tab.n[t];
+        const v4f ds = *reinterpret_cast<const v4f *>(&tab.d[s]);
+        const int4 ns = *reinterpret_cast<const int4 *>(&tab.n[s]);
+        const int nn[4] = {ns.x, ns.y, ns.z, ns.w};
+        b4 hi, lo;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool on = (tb != sb || 4 * g + r <= c) && nn[r] == nt;
+          const float v = on ? p[r] * __builtin_amdgcn_exp2f(dt - ds[r]) : 0.f;
+          hi[r] = from_f32<__bf16>(v);
+          lo[r] = from_f32<__bf16>(v - to_f32(hi[r]));
+        }
+        const int at = tile_at<2>(t, 2 * sb + (g >> 1)) + (g & 1) * 8;
+        *reinterpret_cast<b4 *>(lp + at) = hi;
+        *reinterpret_cast<b4 *>(lpl + at) = lo;
+      }
+      // what the state contributes
+#pragma unroll
+      for (int tb = 0; tb < 4; ++tb)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) O[tb][n] = v4f{0.f, 0.f, 0.f, 0.f};
+      int se[NT];
+      float sf[NT];
+      if constexpr (F16) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float m = 0.f;
+#pragma unroll
+          for (int i = 0; i < 2 * KT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(S[i][n][r]));
+          se[n] = top_exponent(max_over_groups(m));
+          sf[n] = pow2(se[n]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < KT; ++j) {
+        v8 sh[NT], sl[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float v = F16 ? S[2 * j + (e >> 2)][n][e & 3] * sf[n] : S[2 * j + (e >> 2)][n][e & 3];
+            sh[n][e] = from_f32<T>(v);
+            sl[n][e] = from_f32<T>(v - to_f32(sh[n][e]));
+          }
+#pragma unroll
+        for (int tb = 0; tb < 4; ++tb) {
+          const v8 fq = row_operand<T, KT>(lq, 16 * tb + c, j, lane);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            O[tb][n] = Half<T>::mfma16(sh[n], fq, O[tb][n]);
+            O[tb][n] = Half<T>::mfma16(sl[n], fq, O[tb][n]);
+          }
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float back[4] = {1.f, 1.f, 1.f, 1.f};
+        if constexpr (F16) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) back[r] = pow2(-__shfl(se[n], 4 * g + r));  // column 4 g + r is lane 4 g + r's
+        }
+#pragma unroll
+        for (int tb = 0; tb < 4; ++tb) {
+          const float e = tab.e[16 * tb + c];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) O[tb][n][r] *= F16 ? e * back[r] : e;
+        }
+      }
+    }
+    if (more && wave == ((t0 / kBlock) & 3)) make_table(gt, lane, tables[buf ^ 1]);  // the next block's, by each wave in turn
+    if constexpr (!OUT) {
+      G += tab.sum;
+      resets += tab.resets;
+    }
+    if constexpr (OUT) __syncthreads();  // the weights are in LDS
+
+    v8 fv[2][NT];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) fv[kb][n] = column_operand<T, VT>(lv, kb, wave * NT + n, lane);
+    if constexpr (OUT) {
+      b8 vh[2][NT], vl[F16 ? 2 : 1][F16 ? NT : 1];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          if constexpr (F16) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              vh[kb][n][e] = from_f32<__bf16>(to_f32(fv[kb][n][e]));
+              vl[kb][n][e] = from_f32<__bf16>(to_f32(fv[kb][n][e]) - to_f32(vh[kb][n][e]));
+            }
+          } else {
+            vh[kb][n] = fv[kb][n];
+          }
+        }
+#pragma unroll
+      for (int tb = 0; tb < 4; ++tb) {
+#pragma unroll
+        for (int kb = 0; kb <= tb / 2; ++kb) {
+          const b8 ph = row_operand<__bf16, 2>(lp, 16 * tb + c, kb, lane), pl = row_operand<__bf16, 2>(lpl, 16 * tb + c, kb, lane);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            O[tb][n] = Half<__bf16>::mfma16(vh[kb][n], ph, O[tb][n]);
+            O[tb][n] = Half<__bf16>::mfma16(vh[kb][n], pl, O[tb][n]);
+            if constexpr (F16) O[tb][n] = Half<__bf16>::mfma16(vl[kb][n], ph, O[tb][n]);
+          }
+        }
+        const int t = t0 + 16 * tb + c;
+        if (t < t_hi) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const int col = col0 + 16 * n + 4 * g;
+            typename Half<T>::v4 o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(a.scale * O[tb][n][r]);
+            T *to = po + (size_t)t * a.ldo + col;
+            if (col + 4 <= a.dv) {
+              __builtin_memcpy(to, &o, 8);
+            } else {
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (col + r < a.dv) to[r] = o[r];
+            }
+          }
+        }
+      }
+    }
+
+    // the state's update: decay, then k (weighted v)^T
+    constexpr int VP = F16 ? 2 : 3;
+    v8 wv[VP][2][NT];
+    float back[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float x[2][8], m = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const v4f w = *reinterpret_cast<const v4f *>(&tab.w[32 * kb + 16 * hf + 4 * g]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            x[kb][4 * hf + r] = w[r] * to_f32(fv[kb][n][4 * hf + r]);
+            if constexpr (F16) m = fmaxf(m, fabsf(x[kb][4 * hf + r]));
+          }
+        }
+      float up = 1.f;
+      if constexpr (F16) {
+        const int e = top_exponent(max_over_groups(m));
+        up = pow2(e);
+        back[n] = pow2(-e);
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float v = F16 ? x[kb][e] * up : x[kb][e];
+#pragma unroll
+          for (int p = 0; p < VP; ++p) {
+            wv[p][kb][n][e] = from_f32<T>(v);
+            v -= to_f32(wv[p][kb][n][e]);
+          }
+        }
+    }
+    const float dh = tab.dec, dl = tab.dec_lo;
+#pragma unroll
+    for (int i = 0; i < 2 * KT; ++i) {
+      const v8 k0 = column_operand<T, KT>(lk, 0, i, lane), k1 = column_operand<T, KT>(lk, 1, i, lane);
+      v4f u[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          S[i][n][r] = fmaf(S[i][n][r], dh, S[i][n][r] * dl);
+          u[n][r] = F16 ? 0.f : S[i][n][r];
+        }
+#pragma unroll
+      for (int p = VP - 1; p >= 0; --p)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          u[n] = Half<T>::mfma16(k0, wv[p][0][n], u[n]);
+          u[n] = Half<T>::mfma16(k1, wv[p][1][n], u[n]);
+        }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[i][n][r] = F16 ? fmaf(u[n][r], back[n], S[i][n][r]) : u[n][r];
+    }
+    __syncthreads();  // everyone is done with this block's tiles
+    if (more) park();
+    __syncthreads();
+  }
+
+  if constexpr (!OUT) {
+    if (part == 0 && tid == 0) {
+      const double dec = resets ? 0.0 : exp2_neg(G);
+      sg.decays[(size_t)slot * sg.segments + seg] = make_float2((float)dec, (float)(dec - (double)(float)dec));
+    }
+  }
+  float *to = !OUT ? sg.slots + ((size_t)slot * sg.segments + seg + 1) * a.dk * a.dv
+                   : (a.state && t_hi == len ? a.state + (size_t)pair * a.dk * a.dv : nullptr);
+  if (to)
+#pragma unroll
+    for (int m = 0; m < 2 * KT; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = 16 * m + 4 * g + r, col = col0 + 16 * n + c;
+          if (row < a.dk && col < a.dv) to[(size_t)row * a.dv + col] = S[m][n][r];
+        }
+}
+
+// The segments' sums of updates joined: slot j becomes the state segment j starts from.  A thread takes one element through all of them.
+__global__ __launch_bounds__(256) void linattn_join_kernel(LinAttnArgs a, SegArgs sg) {
+  const size_t n = (size_t)a.dk * a.dv, i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const int slot = blockIdx.y, pair = sg.pair0 + slot, b = pair / a.Hv;
+  if (i >= n) return;
+  const int span = sg.blocks * kBlock, used = (seq_len(a, b) + span - 1) / span;
+  if (used == 0) return;
+  float *p = sg.slots + (size_t)slot * sg.segments * n + i;
+  const float2 *d = sg.decays + (size_t)slot * sg.segments;
+  float s = a.state ? a.state[(size_t)pair * n + i] : 0.f;
+  p[0] = s;
+  for (int j = 0; j + 1 < used; ++j) {
+    const float2 f = d[j];
+    s = fmaf(s, f.x, fmaf(s, f.y, p[(size_t)(j + 1) * n]));
+    p[(size_t)(j + 1) * n] = s;
+  }
+}
+
+struct AttnPlan {
+  int kt, nt, segments, blocks, group;  // pairs of one launch
+};
+
+AttnPlan plan_prefill(int Bt, int L, int Hv, int dk, int dv) {
+  AttnPlan p{2, 1, 1, 1, 1};
+  if (Bt == 0 || L == 0) return p;
+  p.kt = dk <= 64 ? 2 : (dk <= 128 ? 4 : 8);
+  p.nt = dv > 64 && p.kt < 8 ? 2 : 1;
+  const long long parts = (dv + 64 * p.nt - 1) / (64 * p.nt), pairs = (long long)Bt * Hv, blocks = (L + kBlock - 1LL) / kBlock;
+  p.group = (int)pairs;
+  long long segments = (512 + pairs * parts - 1) / (pairs * parts);
+  if (segments > blocks) segments = blocks;
+  if (segments < 1) segments = 1;
+  p.blocks = (int)((blocks + segments - 1) / segments);
+  p.segments = p.blocks > 0 ? (int)((blocks + p.blocks - 1) / p.blocks) : 1;
+  return p;
+}
+
+size_t slots_bytes(const AttnPlan &p, int dk, int dv) {
+  return p.segments > 1 ? align_up((size_t)p.group * p.segments * dk * dv * sizeof(float), 256) : 0;
+}
+size_t prefill_workspace(const AttnPlan &p, int dk, int dv) {
+  return p.segments > 1 ? slots_bytes(p, dk, dv) + align_up((size_t)p.group * p.segments * sizeof(float2), 256) : 256;
+}
+
+template <typename T, int KT, int NT>
+int run_blocks(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t st) {
+  const int parts = (a.dv + 64 * NT - 1) / (64 * NT), pairs = a.Bt * a.Hv;
+  for (int at = 0; at < pairs; at += p.group) {
+    SegArgs sg{p.segments, p.blocks, at, pairs - at < p.group ? pairs - at : p.group, static_cast<float *>(ws), nullptr};
+    sg.decays = reinterpret_cast<float2 *>(static_cast<char *>(ws) + slots_bytes(p, a.dk, a.dv));
+    const unsigned one = (unsigned)parts * sg.pairs;
+    if (p.segments > 1) {
+      hipLaunchKernelGGL((linattn_blocks_kernel<T, KT, NT, false>), dim3(one * (p.segments - 1)), dim3(256), 0, st, a, sg);
+      QUAMBA_LAUNCH_CHECK();
+      hipLaunchKernelGGL(linattn_join_kernel, dim3((a.dk * a.dv + 255) / 256, sg.pairs), dim3(256), 0, st, a, sg);
+      QUAMBA_LAUNCH_CHECK();
+    }
+    hipLaunchKernelGGL((linattn_blocks_kernel<T, KT, NT, true>), dim3(one * p.segments), dim3(256), 0, st, a, sg);
+    QUAMBA_LAUNCH_CHECK();
+  }
+  return QUAMBA_OK;
+}
+
+template <typename T>
+int run_prefill(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t st) {
+  if (p.kt == 2) return p.nt == 1 ? run_blocks<T, 2, 1>(a, p, ws, st) : run_blocks<T, 2, 2>(a, p, ws, st);
+  if (p.kt == 4) return p.nt == 1 ? run_blocks<T, 4, 1>(a, p, ws, st) : run_blocks<T, 4, 2>(a, p, ws, st);
+  return run_blocks<T, 8, 1>(a, p, ws, st);
+}
+
 int check(const char *what, int type, const LinAttnArgs &a) {
   if (type != QUAMBA_TYPE_F16 && type != QUAMBA_TYPE_BF16) return fail(QUAMBA_EUNSUPPORTED, "%s: operand type %d", what, type);
   if (a.Bt < 0 || a.L < 0 || a.Hk <= 0 || a.Hv <= 0 || a.dk <= 0 || a.dv <= 0)
@@ -95,11 +649,11 @@ using namespace quamba;
 extern "C" {
 
 size_t quamba_linattn_workspace_bytes(int Bt, int L, int Hk, int Hv, int dk, int dv) {
-  if (Bt < 0 || L < 0 || Hk <= 0 || Hv <= 0 || dk <= 0 || dv <= 0) {
+  if (Bt < 0 || L < 0 || Hk <= 0 || Hv <= 0 || dk <= 0 || dv <= 0 || dk > 256 || dv > 1024) {
     fail(QUAMBA_EINVAL, "linattn: Bt=%d L=%d Hk=%d Hv=%d dk=%d dv=%d", Bt, L, Hk, Hv, dk, dv);
     return 0;
   }
-  return 256;
+  return prefill_workspace(plan_prefill(Bt, L, Hv, dk, dv), dk, dv);
 }
 
 int quamba_linattn_prefill(int type, const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, const float *log_decay,
@@ -109,13 +663,10 @@ int quamba_linattn_prefill(int type, const void *q, int ldq, const void *k, int 
   const int rc = check("linattn_prefill", type, a);
   if (rc != QUAMBA_OK || Bt == 0 || L == 0) return rc;
   if (ws && !aligned(ws, 256)) return fail(QUAMBA_EINVAL, "linattn_prefill: workspace must be 256-byte aligned");
-  const dim3 grid((dv + 15) / 16, Hv, Bt);
-  if (type == QUAMBA_TYPE_F16)
-    hipLaunchKernelGGL(linattn_tokens_kernel<_Float16>, grid, dim3(256), 0, as_stream(stream), a);
-  else
-    hipLaunchKernelGGL(linattn_tokens_kernel<__bf16>, grid, dim3(256), 0, as_stream(stream), a);
-  QUAMBA_LAUNCH_CHECK();
-  return QUAMBA_OK;
+  const AttnPlan p = plan_prefill(Bt, L, Hv, dk, dv);
+  if (p.segments > 1 && (!ws || ws_bytes < prefill_workspace(p, dk, dv)))
+    return fail(QUAMBA_EWORKSPACE, "linattn_prefill: workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, prefill_workspace(p, dk, dv));
+  return type == QUAMBA_TYPE_F16 ? run_prefill<_Float16>(a, p, ws, as_stream(stream)) : run_prefill<__bf16>(a, p, ws, as_stream(stream));
 }
 
 int quamba_linattn_step(int type, const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, const float *log_decay,

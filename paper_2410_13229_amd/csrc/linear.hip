@@ -66,19 +66,6 @@ __device__ __forceinline__ int swz(int row, int chunk) {
   else return row * 256 + ((chunk ^ (row & 15)) << 4);
 }
 
-// Eight consecutive elements of a row from element k on, zeros past K.  A 16-byte load at any element's address.
-template <typename T>
-__device__ __forceinline__ typename Half<T>::v8 row8(const T *row, int k, int K) {
-  typename Half<T>::v8 v;
-  if (k + 8 <= K) {
-    __builtin_memcpy(&v, row + k, 16);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = k + e < K ? row[k + e] : static_cast<T>(0.f);
-  }
-  return v;
-}
-
 // A wave's TM x TN tiles of 32 x 32 sums: register r of lane l in tile (i, j) is column n_base + 32 i + 8 (r / 4) + 4 (l / 32)
 // + r % 4 of row m_base + 32 j + l % 32.  A band of 32 rows and up to 64 columns at a time goes through a region of LDS that
 // only this wave uses (fp32, rows 16 bytes further apart than they are long), so that bias, residual and output are
