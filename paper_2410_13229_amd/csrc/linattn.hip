@@ -4,6 +4,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "device_util.h"
 #include "half_util.h"
 
 namespace quamba {
@@ -98,15 +99,16 @@ struct SegArgs {
 struct GTable {  // of a block's 64 tokens
   float d[kBlock];     // log2 decays summed from the token's group of 16 on
   int n[kBlock];       // stretch (resets up to the token)
-  float e[kBlock];     // exp2(G_t), 0 behind a reset
+  float e[kBlock];     // scale exp2(G_t), 0 behind a reset
   float w[kBlock];     // exp2(G_64 - G_s), 0 in front of a reset
   float between[16];   // 4 tb + sb: sums in front of group tb less those in front of group sb
-  float dec, dec_lo;   // exp2(G_64)
-  int resets;
   double sum;          // G_64
+  double carry;        // what the factors applied so far are off by (their exact product over the applied one)
+  float dec;           // the factor of the state
+  int resets;
 };
 
-// 2^x for x <= 0, to 7e-12: a state's decays multiply up over its blocks, so fp32's rounding of one would show after a hundred
+// 2^x for x <= 0, to 7e-12
 __device__ __forceinline__ double exp2_neg(double x) {
   if (!(x > -200.0)) return x == x ? 0.0 : x;
   const double n = __builtin_rint(x), f = (x - n) * 0.69314718055994530942;
@@ -137,8 +139,10 @@ __device__ __forceinline__ double lane_f64(double v, int lane) {
                               (unsigned)__builtin_amdgcn_readlane((int)b, lane));
 }
 
-// One wave, lane = token: the table of a block from the tokens' log decays (0 behind the end).
-__device__ __forceinline__ void make_table(float g, int lane, GTable &t) {
+// One wave, lane = token: the table of a block from the tokens' log decays (0 behind the end).  The state is multiplied by one
+// fp32 factor per block, and the roundings of a hundred equal factors would add up; so each is rounded from the exact one times
+// what the product so far is off by, which keeps the product over any run of blocks within two roundings.
+__device__ __forceinline__ void make_table(float g, float scale, double carry, int lane, GTable &t) {
   const bool reset = g < -87.f;  // exp leaves fp32's normal range: nothing of the past remains
   const double x = reset || g > 0.f ? 0.0 : (double)g * 1.44269504088896340736;
   double d = x;  // inclusive sums inside rows of 16 lanes
@@ -152,55 +156,81 @@ __device__ __forceinline__ void make_table(float g, int lane, GTable &t) {
   const int n = __popcll(m & (~0ull >> (63 - lane))), last = __popcll(m);
   t.d[lane] = (float)d;
   t.n[lane] = n;
-  t.e[lane] = n ? 0.f : __builtin_amdgcn_exp2f((float)G);
+  t.e[lane] = n ? 0.f : scale * __builtin_amdgcn_exp2f((float)G);
   t.w[lane] = n != last ? 0.f : __builtin_amdgcn_exp2f((float)(all - G));
-  const double dec = last ? 0.0 : exp2_neg(all);
+  const double dec = last ? 0.0 : exp2_neg(all) * carry;
+  const float used = (float)dec;
   const int tb = lane >> 2, sb = lane & 3;
   const double bt = tb == 0 ? 0.0 : (tb == 1 ? b1 : (tb == 2 ? b2 : b3)), bs = sb == 0 ? 0.0 : (sb == 1 ? b1 : (sb == 2 ? b2 : b3));
   if (lane < 16) t.between[lane] = (float)(bt - bs);
   if (lane == 0) {
-    t.dec = (float)dec;
-    t.dec_lo = (float)(dec - (double)(float)dec);
-    t.resets = last;
     t.sum = all;
+    t.carry = used > 1e-30f ? dec / (double)used : 1.0;
+    t.dec = used;
+    t.resets = last;
   }
 }
 
 // LDS rows of 32 KT elements whose 16-byte chunks are exchanged so that 16 rows at one chunk, and 8 rows (0-7 or 8-15) at two
-// adjacent chunks (the transposing reads), fall on different banks.
+// adjacent chunks (the transposing reads), fall on different banks.  The exchange depends on the row modulo 16 only.
+template <int KT>
+__device__ __forceinline__ int swap_of(int row) {
+  return KT == 2 ? (((row >> 1) & 3) << 1) | ((row >> 3) & 1) : ((row & 7) << 1) | ((row >> 3) & 1);
+}
 template <int KT>
 __device__ __forceinline__ int tile_at(int row, int chunk) {
-  const int f = KT == 2 ? (((row >> 1) & 3) << 1) | ((row >> 3) & 1) : ((row & 7) << 1) | ((row >> 3) & 1);
-  return row * (64 * KT) + ((chunk ^ f) << 4);
+  return row * (64 * KT) + ((chunk ^ swap_of<KT>(row)) << 4);
+}
+// A wave's own 16 NT columns of v: rows of 32 NT bytes
+template <int NT>
+__device__ __forceinline__ int swap_v(int row) {
+  return NT == 1 ? 0 : ((row >> 2) & 1) << 1;
+}
+// The block's weights, tokens t x tokens s, on and below the diagonal: 32 columns s for the first 32 rows, 64 for the others
+constexpr int kWeightBytes = 32 * 64 + 32 * 128;
+__device__ __forceinline__ int weight_at(int t, int chunk) {
+  return t < 32 ? t * 64 + ((chunk ^ ((t >> 2) & 3)) << 4) : 2048 + (t - 32) * 128 + ((chunk ^ swap_of<2>(t)) << 4);
 }
 
 typedef short v4s __attribute__((ext_vector_type(4)));
-// Four elements of column `lane % 16` of a 16-column block: rows row0 .. row0 + 3, row0 = 4 (lane / 16) + first.  Each lane
-// points at 4 elements of one row; the read exchanges them inside groups of 16 lanes.
-template <typename T, int KT>
-__device__ __forceinline__ typename Half<T>::v4 read_columns(const char *tile, int first, int block, int lane) {
-  const int i = lane & 15, row = first + 4 * (lane >> 4) + (i >> 2), chunk = 2 * block + ((i & 3) >> 1);
-  const char *p = tile + tile_at<KT>(row, chunk) + (i & 1) * 8;
+// Four elements of column `lane % 16` of a block of 16 columns, rows first + 4 (lane / 16) .. + 3: each lane points at 4 elements
+// of one row, and the read exchanges them inside groups of 16 lanes.
+template <typename T>
+__device__ __forceinline__ typename Half<T>::v4 read_exchanged(const char *p) {
   const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3))) *)(p));
   return __builtin_bit_cast(typename Half<T>::v4, r);
+}
+template <typename V4>
+__device__ __forceinline__ auto both(V4 lo, V4 hi) {
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 // Operand of 32 rows (tokens) of a column block: rows 32 kb + 16 a + 4 g + r in slot 4 a + r of lane group g
 template <typename T, int KT>
 __device__ __forceinline__ typename Half<T>::v8 column_operand(const char *tile, int kb, int block, int lane) {
-  const auto lo = read_columns<T, KT>(tile, 32 * kb, block, lane), hi = read_columns<T, KT>(tile, 32 * kb + 16, block, lane);
-  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  const int i = lane & 15, row = 32 * kb + 4 * (lane >> 4) + (i >> 2), chunk = 2 * block + ((i & 3) >> 1), off = (i & 1) * 8;
+  return both(read_exchanged<T>(tile + tile_at<KT>(row, chunk) + off), read_exchanged<T>(tile + tile_at<KT>(row + 16, chunk) + off));
+}
+template <typename T, int NT>
+__device__ __forceinline__ typename Half<T>::v8 value_operand(const char *own, int kb, int n, int lane) {
+  const int i = lane & 15, row = 32 * kb + 4 * (lane >> 4) + (i >> 2), chunk = 2 * n + ((i & 3) >> 1);
+  const char *p = own + row * (32 * NT) + ((chunk ^ swap_v<NT>(row)) << 4) + (i & 1) * 8;
+  return both(read_exchanged<T>(p), read_exchanged<T>(p + 16 * 32 * NT));  // 16 rows on: the same exchange
 }
 // Operand of one row: elements 32 j + 16 a + 4 g + r in slot 4 a + r
 template <typename T, int KT>
 __device__ __forceinline__ typename Half<T>::v8 row_operand(const char *tile, int row, int j, int lane) {
   const int g = lane >> 4, chunk = 4 * j + (g >> 1), off = (g & 1) * 8;
-  const auto lo = *reinterpret_cast<const typename Half<T>::v4 *>(tile + tile_at<KT>(row, chunk) + off);
-  const auto hi = *reinterpret_cast<const typename Half<T>::v4 *>(tile + tile_at<KT>(row, chunk + 2) + off);
-  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  typedef typename Half<T>::v4 v4;
+  return both(*reinterpret_cast<const v4 *>(tile + tile_at<KT>(row, chunk) + off), *reinterpret_cast<const v4 *>(tile + tile_at<KT>(row, chunk + 2) + off));
+}
+__device__ __forceinline__ Half<__bf16>::v8 weight_operand(const char *p, int t, int kb, int lane) {
+  const int g = lane >> 4, chunk = 4 * kb + (g >> 1), off = (g & 1) * 8;
+  typedef Half<__bf16>::v4 v4;
+  return both(*reinterpret_cast<const v4 *>(p + weight_at(t, chunk) + off), *reinterpret_cast<const v4 *>(p + weight_at(t, chunk + 2) + off));
 }
 
-// 2^-(exponent of m) brought to the top of fp16's range (2^12 .. 2^13), its exponent limited so that it stays an ordinary fp32
-// number; m = 0 and m = infinity or NaN too
+// The power of two (its exponent) that brings m to 2^12 .. 2^13, the top of fp16's range, limited so that it stays an ordinary
+// fp32 number
 __device__ __forceinline__ int top_exponent(float m) {
   const int e = 127 + 12 - (int)((__float_as_uint(m) >> 23) & 0xff);
   return min(max(e, -100), 100);
@@ -214,18 +244,37 @@ __device__ __forceinline__ float max_over_groups(float m) {
 
 __device__ __forceinline__ int seq_len(const LinAttnArgs &a, int b) { return a.lens ? min(max(a.lens[b], 0), a.L) : a.L; }
 
-// KT: dk <= 32 KT.  OUT: outputs and the state; otherwise only a segment's own sum of updates and its decay.
-template <typename T, int KT, int NT, bool OUT>
-__global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, SegArgs sg) {
+// 16 bytes a lane from base + off (lane) + soff (wave) to consecutive LDS from `to` on; zeros where off is past the buffer
+__device__ __forceinline__ void load_to_lds(const void *base, int off, int soff, char *to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_over(base, 0x7fffffff), (void __attribute__((address_space(3))) *)to, 16, off, soff, 0, 0);
+}
+
+// Order LDS accesses (the compiler's and the wave's own) around the hardware barrier.  VM: the wave's direct-to-LDS loads have
+// landed too.
+template <bool VM>
+__device__ __forceinline__ void block_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(VM ? 0x0070 : 0xC07F);  // (vmcnt 0 and) lgkmcnt 0, the rest not waited for
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// KT: dk <= 32 KT.  OUT: outputs and the state; otherwise only a segment's own sum of updates and its decay.  WIDE: rows and
+// heads start on 16 bytes and a block's rows span less than 2^31 bytes: tiles travel by direct-to-LDS buffer loads, whose lanes
+// behind the end or behind dk or dv get an offset past the buffer and leave zeros.  Otherwise they pass through registers.
+//
+// LDS for two workgroups on a CU (KT = 4, NT = 2: 78.5 of 80 KB): k twice, the next block's arriving while this one's is used; q
+// and v once: q is done with at the barrier behind the weights, v belongs to one wave and is done with once it is in registers.
+template <typename T, int KT, int NT, bool OUT, bool WIDE>
+__global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_kernel(LinAttnArgs a, SegArgs sg) {
   constexpr bool F16 = std::is_same<T, _Float16>::value;
-  constexpr int VT = 2 * NT;                                  // 32-element blocks of a row of v: 64 NT columns
-  constexpr int QB = OUT ? 64 * KT * kBlock : 0, KB = 64 * KT * kBlock, VB = 64 * VT * kBlock, PB = OUT ? 128 * kBlock : 0;
+  constexpr int TB = 64 * KT * kBlock, VB = 32 * NT * kBlock, QB = OUT ? TB : 0;  // bytes of a k or q tile, of a wave's v
   typedef typename Half<T>::v8 v8;
   typedef Half<__bf16>::v8 b8;
   typedef Half<__bf16>::v4 b4;
-  __shared__ __attribute__((aligned(16))) char lds[QB + KB + VB + 2 * PB];
+  __shared__ __attribute__((aligned(16))) char lds[QB + 2 * TB + 4 * VB + (OUT ? 2 * kWeightBytes : 0)];
   __shared__ GTable tables[2];
-  char *lq = lds, *lk = lds + QB, *lv = lk + KB, *lp = lv + VB, *lpl = lp + PB;
+  char *lq = lds, *lks = lds + QB, *lvs = lks + 2 * TB, *lp = lvs + 4 * VB, *lpl = lp + kWeightBytes;
 
   // XCDs get contiguous runs of workgroups (ids are dealt round-robin to the 8 of them): column parts of a head, heads of a
   // segment next to one another, so what shares q and k shares an L2
@@ -242,50 +291,76 @@ __global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, S
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col0 = part * 64 * NT + wave * 16 * NT;  // this wave's first column
+  char *lv = lvs + wave * VB;
 
   const size_t row0 = (size_t)b * a.L;
   const T *pq = static_cast<const T *>(a.q) + row0 * a.ldq + (size_t)hk * a.dk;
   const T *pk = static_cast<const T *>(a.k) + row0 * a.ldk + (size_t)hk * a.dk;
-  const T *pv = static_cast<const T *>(a.v) + row0 * a.ldv + (size_t)h * a.dv + part * 64 * NT;
-  const int dv_part = a.dv - part * 64 * NT;
+  const T *pv = static_cast<const T *>(a.v) + row0 * a.ldv + (size_t)h * a.dv;
   T *po = static_cast<T *>(a.out) + row0 * a.ldo + (size_t)h * a.dv;
 
-  // a block's rows, 16 bytes a lane along them: zeros behind the end and behind dk or dv
-  constexpr int CPK = 4 * KT, CPV = 4 * VT, NK = kBlock * CPK / 256, NV = kBlock * CPV / 256;
-  v8 rq[OUT ? NK : 1], rk[NK], rv[NV];
+  // A wave-level load fills 1 KB of LDS, 16 bytes a lane: a k or q tile in NL loads of each wave, whose rows differ by PH loads in
+  // multiples of 16, so that PH lane offsets serve all of them; a wave's v in NLV loads.
+  constexpr int RPL = 16 / KT, NL = KT, PH = 4 * RPL >= 16 ? 1 : 16 / (4 * RPL), RPLV = 32 / NT, NLV = 2 * NT;
+  auto tile_row = [&](int i) { return (i / PH) * (PH * 4 * RPL) + (i % PH) * 4 * RPL + wave * RPL + lane / (64 / RPL); };
+  auto tile_chunk = [&](int i) { return (lane % (64 / RPL)) ^ swap_of<KT>(tile_row(i)); };
+  const int v_row = lane / (2 * NT), v_chunk = (lane % (2 * NT)) ^ swap_v<NT>(v_row);  // of load 0; RPLV rows further with each
+  constexpr int OFF = (int)0x80000000;  // past every buffer
+  int oq[PH], ok[PH], ov;
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int i = 0; i < PH; ++i) {
+      const bool in = tile_chunk(i) * 8 < a.dk;
+      oq[i] = in ? (int)(tile_row(i) * a.ldq + tile_chunk(i) * 8) * 2 : OFF;
+      ok[i] = in ? (int)(tile_row(i) * a.ldk + tile_chunk(i) * 8) * 2 : OFF;
+    }
+    ov = col0 + v_chunk * 8 < a.dv ? (int)(v_row * a.ldv + col0 + v_chunk * 8) * 2 : OFF;
+  }
+  v8 rq[!WIDE && OUT ? NL : 1], rk[!WIDE ? NL : 1], rv[!WIDE ? NLV : 1];
   const v8 zero = {};
-  float gt = 0.f;
-  auto fetch = [&](int t0) {
+  auto fetch_tile = [&](const T *p, long long ld, const int (&o)[PH], v8 *r, int t0, char *tile) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const int ch = tid + 256 * i, t = t0 + ch / CPK, e = ch % CPK * 8;
-      if constexpr (OUT) rq[i] = t < t_hi ? row8(pq + (size_t)t * a.ldq, e, a.dk) : zero;
-      rk[i] = t < t_hi ? row8(pk + (size_t)t * a.ldk, e, a.dk) : zero;
+    for (int i = 0; i < NL; ++i) {
+      const int n = t_hi - t0;  // rows that count
+      if constexpr (WIDE) {
+        const int off = n >= kBlock || tile_row(i) < n ? o[i % PH] : OFF;
+        load_to_lds(p + (size_t)t0 * ld, off, (int)((i / PH) * (PH * 4 * RPL) * ld * 2), tile + ((i / PH) * PH * 4 + (i % PH) * 4 + wave) * 1024);
+      } else {
+        r[i] = tile_row(i) < n ? row8(p + (size_t)(t0 + tile_row(i)) * ld, tile_chunk(i) * 8, a.dk) : zero;
+      }
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int ch = tid + 256 * i, t = t0 + ch / CPV, e = ch % CPV * 8;
-      rv[i] = t < t_hi ? row8(pv + (size_t)t * a.ldv, e, dv_part) : zero;
-    }
-    gt = 0.f;
-    const int t = t0 + lane;
-    if (a.g && t < t_hi) gt = a.ldg ? a.g[(row0 + t) * a.ldg + h] : a.g[h];
   };
-  auto park = [&]() {
+  auto fetch_v = [&](int t0) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const int ch = tid + 256 * i;
-      if constexpr (OUT) *reinterpret_cast<v8 *>(lq + tile_at<KT>(ch / CPK, ch % CPK)) = rq[i];
-      *reinterpret_cast<v8 *>(lk + tile_at<KT>(ch / CPK, ch % CPK)) = rk[i];
+    for (int i = 0; i < NLV; ++i) {
+      const int n = t_hi - t0, row = v_row + RPLV * i;
+      if constexpr (WIDE)
+        load_to_lds(pv + (size_t)t0 * a.ldv, n >= kBlock || row < n ? ov : OFF, (int)(RPLV * i * a.ldv * 2), lv + i * 1024);
+      else
+        rv[i] = row < n ? row8(pv + (size_t)(t0 + row) * a.ldv, col0 + v_chunk * 8, a.dv) : zero;
     }
+  };
+  auto park = [&](char *lk) {  // what came through registers
+    if constexpr (!WIDE) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int ch = tid + 256 * i;
-      *reinterpret_cast<v8 *>(lv + tile_at<VT>(ch / CPV, ch % CPV)) = rv[i];
+      for (int i = 0; i < NL; ++i) {
+        const int at = ((i / PH) * PH * 4 + (i % PH) * 4 + wave) * 1024 + lane * 16;
+        if constexpr (OUT) *reinterpret_cast<v8 *>(lq + at) = rq[i];
+        *reinterpret_cast<v8 *>(lk + at) = rk[i];
+      }
+#pragma unroll
+      for (int i = 0; i < NLV; ++i) *reinterpret_cast<v8 *>(lv + i * 1024 + lane * 16) = rv[i];
     }
+  };
+  auto log_decay = [&](int t0) {
+    const int t = t0 + lane;
+    return a.g && t < t_hi ? (a.ldg ? a.g[(row0 + t) * a.ldg + h] : a.g[h]) : 0.f;
   };
 
-  fetch(t_lo);
+  fetch_tile(pk, a.ldk, ok, rk, t_lo, lks);
+  if constexpr (OUT) fetch_tile(pq, a.ldq, oq, rq, t_lo, lq);
+  fetch_v(t_lo);
+  float gt = log_decay(t_lo);
 
   // S[m][n]: rows 16 m + 4 g + r of column col0 + 16 n + c
   v4f S[2 * KT][NT];
@@ -302,23 +377,33 @@ __global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, S
       }
 
   if constexpr (OUT) {
-    // the blocks of weights above the diagonal that a product of 32 tokens takes in: zero, and never written again
-    for (int i = tid; i < 2 * 2 * 16 * 2; i += 256) {  // piece, block pair, row, chunk
-      const int piece = i & 1, pr = (i >> 1) & 1, row = 32 * pr + ((i >> 2) & 15), chunk = 4 * pr + 2 + (i >> 6);
-      *reinterpret_cast<b8 *>((piece ? lpl : lp) + tile_at<2>(row, chunk)) = b8{};
+    // the weights above the diagonal that a product of 32 tokens takes in: zero, and never written again
+    if (tid < 128) {  // piece, which of two, row, chunk
+      const int pr = (tid >> 1) & 1, row = 32 * pr + ((tid >> 2) & 15), chunk = 4 * pr + 2 + (tid >> 6);
+      *reinterpret_cast<b8 *>((tid & 1 ? lpl : lp) + weight_at(row, chunk)) = b8{};
     }
   }
   double G = 0.0;  // of the segment
   int resets = 0;
-  if (wave == 0) make_table(gt, lane, tables[0]);
-  park();
-  __syncthreads();
+  if (wave == 0) make_table(gt, a.scale, 1.0, lane, tables[0]);
+  park(lks);
+  block_barrier<true>();
 
   int buf = 0;
   for (int t0 = t_lo; t0 < t_hi; t0 += kBlock, buf ^= 1) {
     const GTable &tab = tables[buf];
-    const bool more = t0 + kBlock < t_hi;
-    if (more) fetch(t0 + kBlock);
+    const char *lk = lks + buf * TB;
+    char *lk_next = lks + (buf ^ 1) * TB;
+    const int t1 = t0 + kBlock;
+    const bool more = t1 < t_hi;
+    if (more) {
+      fetch_tile(pk, a.ldk, ok, rk, t1, lk_next);
+      if constexpr (!WIDE) {
+        if constexpr (OUT) fetch_tile(pq, a.ldq, oq, rq, t1, lq);
+        fetch_v(t1);
+      }
+      gt = log_decay(t1);
+    }
 
     v4f O[4][NT];  // transposed: columns (of v) 4 g + r, token 16 tb + c
     if constexpr (OUT) {
@@ -342,11 +427,11 @@ __global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, S
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const bool on = (tb != sb || 4 * g + r <= c) && nn[r] == nt;
-          const float v = on ? p[r] * __builtin_amdgcn_exp2f(dt - ds[r]) : 0.f;
+          const float v = on ? a.scale * p[r] * __builtin_amdgcn_exp2f(dt - ds[r]) : 0.f;
           hi[r] = from_f32<__bf16>(v);
           lo[r] = from_f32<__bf16>(v - to_f32(hi[r]));
         }
-        const int at = tile_at<2>(t, 2 * sb + (g >> 1)) + (g & 1) * 8;
+        const int at = weight_at(t, 2 * sb + (g >> 1)) + (g & 1) * 8;
         *reinterpret_cast<b4 *>(lp + at) = hi;
         *reinterpret_cast<b4 *>(lpl + at) = lo;
       }
@@ -405,18 +490,30 @@ __global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, S
         }
       }
     }
-    if (more && wave == ((t0 / kBlock) & 3)) make_table(gt, lane, tables[buf ^ 1]);  // the next block's, by each wave in turn
+    if (more && wave == ((t0 / kBlock) & 3)) make_table(gt, a.scale, tab.carry, lane, tables[buf ^ 1]);  // the next block's, by each wave in turn
     if constexpr (!OUT) {
       G += tab.sum;
       resets += tab.resets;
     }
-    if constexpr (OUT) __syncthreads();  // the weights are in LDS
+    if constexpr (OUT) {
+      block_barrier<false>();  // the weights are in LDS, q is done with
+      if (WIDE && more) fetch_tile(pq, a.ldq, oq, rq, t1, lq);
+    }
 
     v8 fv[2][NT];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) fv[kb][n] = column_operand<T, VT>(lv, kb, wave * NT + n, lane);
+      for (int n = 0; n < NT; ++n) {
+        fv[kb][n] = value_operand<T, NT>(lv, kb, n, lane);
+      }
+    if (WIDE && more) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) asm volatile("" : "+v"(fv[kb][n])::"memory");  // read before the next block's may arrive
+      fetch_v(t1);
+    }
     if constexpr (OUT) {
       b8 vh[2][NT], vl[F16 ? 2 : 1][F16 ? NT : 1];
 #pragma unroll
@@ -437,7 +534,7 @@ __global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, S
       for (int tb = 0; tb < 4; ++tb) {
 #pragma unroll
         for (int kb = 0; kb <= tb / 2; ++kb) {
-          const b8 ph = row_operand<__bf16, 2>(lp, 16 * tb + c, kb, lane), pl = row_operand<__bf16, 2>(lpl, 16 * tb + c, kb, lane);
+          const b8 ph = weight_operand(lp, 16 * tb + c, kb, lane), pl = weight_operand(lpl, 16 * tb + c, kb, lane);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             O[tb][n] = Half<__bf16>::mfma16(vh[kb][n], ph, O[tb][n]);
@@ -452,11 +549,11 @@ __global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, S
             const int col = col0 + 16 * n + 4 * g;
             typename Half<T>::v4 o;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(a.scale * O[tb][n][r]);
+            for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(O[tb][n][r]);
             T *to = po + (size_t)t * a.ldo + col;
             if (col + 4 <= a.dv) {
               __builtin_memcpy(to, &o, 8);
-            } else {
+            } else if constexpr (!WIDE) {
 #pragma unroll
               for (int r = 0; r < 4; ++r)
                 if (col + r < a.dv) to[r] = o[r];
@@ -502,7 +599,7 @@ __global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, S
           }
         }
     }
-    const float dh = tab.dec, dl = tab.dec_lo;
+    const float dec = tab.dec;
 #pragma unroll
     for (int i = 0; i < 2 * KT; ++i) {
       const v8 k0 = column_operand<T, KT>(lk, 0, i, lane), k1 = column_operand<T, KT>(lk, 1, i, lane);
@@ -510,10 +607,7 @@ __global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, S
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          S[i][n][r] = fmaf(S[i][n][r], dh, S[i][n][r] * dl);
-          u[n][r] = F16 ? 0.f : S[i][n][r];
-        }
+        for (int r = 0; r < 4; ++r) u[n][r] = F16 ? 0.f : S[i][n][r] * dec;
 #pragma unroll
       for (int p = VP - 1; p >= 0; --p)
 #pragma unroll
@@ -524,11 +618,10 @@ __global__ __launch_bounds__(256, 2) void linattn_blocks_kernel(LinAttnArgs a, S
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[i][n][r] = F16 ? fmaf(u[n][r], back[n], S[i][n][r]) : u[n][r];
+        for (int r = 0; r < 4; ++r) S[i][n][r] = F16 ? fmaf(u[n][r], back[n], S[i][n][r] * dec) : u[n][r];
     }
-    __syncthreads();  // everyone is done with this block's tiles
-    if (more) park();
-    __syncthreads();
+    if (more) park(lk_next);
+    block_barrier<true>();  // the next block's tiles are in LDS, this one's are done with
   }
 
   if constexpr (!OUT) {
@@ -580,7 +673,7 @@ AttnPlan plan_prefill(int Bt, int L, int Hv, int dk, int dv) {
   p.nt = dv > 64 && p.kt < 8 ? 2 : 1;
   const long long parts = (dv + 64 * p.nt - 1) / (64 * p.nt), pairs = (long long)Bt * Hv, blocks = (L + kBlock - 1LL) / kBlock;
   p.group = (int)pairs;
-  long long segments = (512 + pairs * parts - 1) / (pairs * parts);
+  long long segments = 512 / (pairs * parts);
   if (segments > blocks) segments = blocks;
   if (segments < 1) segments = 1;
   p.blocks = (int)((blocks + segments - 1) / segments);
@@ -595,7 +688,7 @@ size_t prefill_workspace(const AttnPlan &p, int dk, int dv) {
   return p.segments > 1 ? slots_bytes(p, dk, dv) + align_up((size_t)p.group * p.segments * sizeof(float2), 256) : 256;
 }
 
-template <typename T, int KT, int NT>
+template <typename T, int KT, int NT, bool WIDE>
 int run_blocks(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t st) {
   const int parts = (a.dv + 64 * NT - 1) / (64 * NT), pairs = a.Bt * a.Hv;
   for (int at = 0; at < pairs; at += p.group) {
@@ -603,22 +696,29 @@ int run_blocks(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t st
     sg.decays = reinterpret_cast<float2 *>(static_cast<char *>(ws) + slots_bytes(p, a.dk, a.dv));
     const unsigned one = (unsigned)parts * sg.pairs;
     if (p.segments > 1) {
-      hipLaunchKernelGGL((linattn_blocks_kernel<T, KT, NT, false>), dim3(one * (p.segments - 1)), dim3(256), 0, st, a, sg);
+      hipLaunchKernelGGL((linattn_blocks_kernel<T, KT, NT, false, WIDE>), dim3(one * (p.segments - 1)), dim3(256), 0, st, a, sg);
       QUAMBA_LAUNCH_CHECK();
       hipLaunchKernelGGL(linattn_join_kernel, dim3((a.dk * a.dv + 255) / 256, sg.pairs), dim3(256), 0, st, a, sg);
       QUAMBA_LAUNCH_CHECK();
     }
-    hipLaunchKernelGGL((linattn_blocks_kernel<T, KT, NT, true>), dim3(one * p.segments), dim3(256), 0, st, a, sg);
+    hipLaunchKernelGGL((linattn_blocks_kernel<T, KT, NT, true, WIDE>), dim3(one * p.segments), dim3(256), 0, st, a, sg);
     QUAMBA_LAUNCH_CHECK();
   }
   return QUAMBA_OK;
 }
 
-template <typename T>
+template <typename T, bool WIDE>
 int run_prefill(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t st) {
-  if (p.kt == 2) return p.nt == 1 ? run_blocks<T, 2, 1>(a, p, ws, st) : run_blocks<T, 2, 2>(a, p, ws, st);
-  if (p.kt == 4) return p.nt == 1 ? run_blocks<T, 4, 1>(a, p, ws, st) : run_blocks<T, 4, 2>(a, p, ws, st);
-  return run_blocks<T, 8, 1>(a, p, ws, st);
+  if (p.kt == 2) return p.nt == 1 ? run_blocks<T, 2, 1, WIDE>(a, p, ws, st) : run_blocks<T, 2, 2, WIDE>(a, p, ws, st);
+  if (p.kt == 4) return p.nt == 1 ? run_blocks<T, 4, 1, WIDE>(a, p, ws, st) : run_blocks<T, 4, 2, WIDE>(a, p, ws, st);
+  return run_blocks<T, 8, 1, WIDE>(a, p, ws, st);
+}
+
+// Rows that the direct-to-LDS loads can take: every row and head starts on 16 bytes, 64 rows lie within 2^31 bytes.
+bool wide_rows(const LinAttnArgs &a) {
+  const long long most = 1LL << 23;
+  return aligned(a.q, 16) && aligned(a.k, 16) && aligned(a.v, 16) && a.ldq % 8 == 0 && a.ldk % 8 == 0 && a.ldv % 8 == 0 && a.dk % 8 == 0 &&
+         a.dv % 8 == 0 && a.ldq < most && a.ldk < most && a.ldv < most;
 }
 
 int check(const char *what, int type, const LinAttnArgs &a) {
@@ -666,7 +766,9 @@ int quamba_linattn_prefill(int type, const void *q, int ldq, const void *k, int 
   const AttnPlan p = plan_prefill(Bt, L, Hv, dk, dv);
   if (p.segments > 1 && (!ws || ws_bytes < prefill_workspace(p, dk, dv)))
     return fail(QUAMBA_EWORKSPACE, "linattn_prefill: workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, prefill_workspace(p, dk, dv));
-  return type == QUAMBA_TYPE_F16 ? run_prefill<_Float16>(a, p, ws, as_stream(stream)) : run_prefill<__bf16>(a, p, ws, as_stream(stream));
+  hipStream_t st = as_stream(stream);
+  if (type == QUAMBA_TYPE_F16) return wide_rows(a) ? run_prefill<_Float16, true>(a, p, ws, st) : run_prefill<_Float16, false>(a, p, ws, st);
+  return wide_rows(a) ? run_prefill<__bf16, true>(a, p, ws, st) : run_prefill<__bf16, false>(a, p, ws, st);
 }
 
 int quamba_linattn_step(int type, const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, const float *log_decay,
