@@ -204,11 +204,18 @@ template <typename V4>
 __device__ __forceinline__ auto both(V4 lo, V4 hi) {
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
-// Operand of 32 rows (tokens) of a column block: rows 32 kb + 16 a + 4 g + r in slot 4 a + r of lane group g
+// Operand of 32 rows (tokens) of a column block, rows 32 kb + 16 a + 4 g + r in slot 4 a + r of lane group g.  Of a k tile:
+// column_at is the lane's offset of block 0; a block is an exclusive-or away (the exchange moves chunks by exclusive-or too),
+// 16 rows a constant.
+template <int KT>
+__device__ __forceinline__ int column_at(int lane) {
+  const int i = lane & 15, row = 4 * (lane >> 4) + (i >> 2);
+  return tile_at<KT>(row, (i & 3) >> 1) + (i & 1) * 8;
+}
 template <typename T, int KT>
-__device__ __forceinline__ typename Half<T>::v8 column_operand(const char *tile, int kb, int block, int lane) {
-  const int i = lane & 15, row = 32 * kb + 4 * (lane >> 4) + (i >> 2), chunk = 2 * block + ((i & 3) >> 1), off = (i & 1) * 8;
-  return both(read_exchanged<T>(tile + tile_at<KT>(row, chunk) + off), read_exchanged<T>(tile + tile_at<KT>(row + 16, chunk) + off));
+__device__ __forceinline__ typename Half<T>::v8 column_operand(const char *tiles, int at, int kb, int block) {
+  const char *p = tiles + (at ^ (block << 5)) + 32 * kb * 64 * KT;
+  return both(read_exchanged<T>(p), read_exchanged<T>(p + 16 * 64 * KT));
 }
 template <typename T, int NT>
 __device__ __forceinline__ typename Half<T>::v8 value_operand(const char *own, int kb, int n, int lane) {
@@ -216,12 +223,17 @@ __device__ __forceinline__ typename Half<T>::v8 value_operand(const char *own, i
   const char *p = own + row * (32 * NT) + ((chunk ^ swap_v<NT>(row)) << 4) + (i & 1) * 8;
   return both(read_exchanged<T>(p), read_exchanged<T>(p + 16 * 32 * NT));  // 16 rows on: the same exchange
 }
-// Operand of one row: elements 32 j + 16 a + 4 g + r in slot 4 a + r
+// Operand of one row, elements 32 j + 16 a + 4 g + r in slot 4 a + r.  row_at: the lane's offset in row lane % 16 for j = 0
+template <int KT>
+__device__ __forceinline__ int row_at(int lane) {
+  const int g = lane >> 4;
+  return tile_at<KT>(lane & 15, g >> 1) + (g & 1) * 8;
+}
 template <typename T, int KT>
-__device__ __forceinline__ typename Half<T>::v8 row_operand(const char *tile, int row, int j, int lane) {
-  const int g = lane >> 4, chunk = 4 * j + (g >> 1), off = (g & 1) * 8;
+__device__ __forceinline__ typename Half<T>::v8 row_operand(const char *tile, int at, int tb, int j) {
   typedef typename Half<T>::v4 v4;
-  return both(*reinterpret_cast<const v4 *>(tile + tile_at<KT>(row, chunk) + off), *reinterpret_cast<const v4 *>(tile + tile_at<KT>(row, chunk + 2) + off));
+  const char *p = tile + 16 * tb * 64 * KT;
+  return both(*reinterpret_cast<const v4 *>(p + (at ^ (j << 6))), *reinterpret_cast<const v4 *>(p + (at ^ (j << 6) ^ 32)));
 }
 __device__ __forceinline__ Half<__bf16>::v8 weight_operand(const char *p, int t, int kb, int lane) {
   const int g = lane >> 4, chunk = 4 * kb + (g >> 1), off = (g & 1) * 8;
@@ -248,6 +260,29 @@ __device__ __forceinline__ int seq_len(const LinAttnArgs &a, int b) { return a.l
 __device__ __forceinline__ void load_to_lds(const void *base, int off, int soff, char *to) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_over(base, 0x7fffffff), (void __attribute__((address_space(3))) *)to, 16, off, soff, 0, 0);
 }
+
+// Two fp32 values as one word of 16-bit ones, rounded to nearest
+template <typename T>
+__device__ __forceinline__ unsigned pack2(float a, float b) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef T t2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{a, b}), t2));
+}
+// The same, and what it leaves over.  fp16 takes its first piece by truncation, which packs
+// in one instruction; the last piece of a value is always rounded to nearest (pack2).
+__device__ __forceinline__ unsigned take2(float &a, float &b, __bf16) {
+  const unsigned w = pack2<__bf16>(a, b);
+  a -= __uint_as_float(w << 16);
+  b -= __uint_as_float(w & 0xffff0000u);
+  return w;
+}
+__device__ __forceinline__ unsigned take2(float &a, float &b, _Float16) {
+  const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
+  a -= static_cast<float>(h[0]);
+  b -= static_cast<float>(h[1]);
+  return __builtin_bit_cast(unsigned, h);
+}
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
 // Order LDS accesses (the compiler's and the wave's own) around the hardware barrier.  VM: the wave's direct-to-LDS loads have
 // landed too.
@@ -306,7 +341,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
   auto tile_chunk = [&](int i) { return (lane % (64 / RPL)) ^ swap_of<KT>(tile_row(i)); };
   const int v_row = lane / (2 * NT), v_chunk = (lane % (2 * NT)) ^ swap_v<NT>(v_row);  // of load 0; RPLV rows further with each
   constexpr int OFF = (int)0x80000000;  // past every buffer
-  int oq[PH], ok[PH], ov;
+  int oq[PH], ok[PH], ov, oo[NT];
   if constexpr (WIDE) {
 #pragma unroll
     for (int i = 0; i < PH; ++i) {
@@ -314,6 +349,8 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
       oq[i] = in ? (int)(tile_row(i) * a.ldq + tile_chunk(i) * 8) * 2 : OFF;
       ok[i] = in ? (int)(tile_row(i) * a.ldk + tile_chunk(i) * 8) * 2 : OFF;
     }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) oo[n] = col0 + 16 * n + 4 * g < a.dv ? (int)(c * a.ldo + col0 + 16 * n + 4 * g) * 2 : OFF;
     ov = col0 + v_chunk * 8 < a.dv ? (int)(v_row * a.ldv + col0 + v_chunk * 8) * 2 : OFF;
   }
   v8 rq[!WIDE && OUT ? NL : 1], rk[!WIDE ? NL : 1], rv[!WIDE ? NLV : 1];
@@ -392,7 +429,10 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
   int buf = 0;
   for (int t0 = t_lo; t0 < t_hi; t0 += kBlock, buf ^= 1) {
     const GTable &tab = tables[buf];
-    const char *lk = lks + buf * TB;
+    // the lane's offsets in the tiles, opaque so that the exclusive-ors of the operand reads stay where they are used: hoisted out of
+    // the loop they take 30 registers
+    int at_row = row_at<KT>(lane), at_column = column_at<KT>(lane) + buf * TB, at_chunk = tile_at<KT>(c, g);
+    asm volatile("" : "+v"(at_row), "+v"(at_column), "+v"(at_chunk));
     char *lk_next = lks + (buf ^ 1) * TB;
     const int t1 = t0 + kBlock;
     const bool more = t1 < t_hi;
@@ -407,14 +447,16 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 
     v4f O[4][NT];  // transposed: columns (of v) 4 g + r, token 16 tb + c
     if constexpr (OUT) {
-      // weights: 10 blocks of 16 x 16 on and below the diagonal, dealt to the waves
-      for (int id10 = wave; id10 < 10; id10 += 4) {
+      // weights: the 10 blocks of 16 x 16 on and below the diagonal, three for waves 0 and 1, two for waves 2 and 3, which make the
+      // next block's table in turn
+      auto weights = [&](int id10) {
         const int tb = id10 < 1 ? 0 : (id10 < 3 ? 1 : (id10 < 6 ? 2 : 3)), sb = id10 - tb * (tb + 1) / 2;
         v4f p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < KT; ++j) {
-          const v8 fk = *reinterpret_cast<const v8 *>(lk + tile_at<KT>(16 * sb + c, 4 * j + g));
-          const v8 fq = *reinterpret_cast<const v8 *>(lq + tile_at<KT>(16 * tb + c, 4 * j + g));
+          const int at = at_chunk ^ (j << 6);
+          const v8 fk = *reinterpret_cast<const v8 *>(lks + buf * TB + 16 * sb * 64 * KT + at);
+          const v8 fq = *reinterpret_cast<const v8 *>(lq + 16 * tb * 64 * KT + at);
           p = Half<T>::mfma16(fk, fq, p);  // rows s, columns t
         }
         const int t = 16 * tb + c, s = 16 * sb + 4 * g;
@@ -423,18 +465,28 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
         const v4f ds = *reinterpret_cast<const v4f *>(&tab.d[s]);
         const int4 ns = *reinterpret_cast<const int4 *>(&tab.n[s]);
         const int nn[4] = {ns.x, ns.y, ns.z, ns.w};
-        b4 hi, lo;
+        const int first = tb != sb ? -1 : 4 * g - c;  // s - t of r = 0, or anything negative enough
+        float v[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool on = (tb != sb || 4 * g + r <= c) && nn[r] == nt;
-          const float v = on ? a.scale * p[r] * __builtin_amdgcn_exp2f(dt - ds[r]) : 0.f;
-          hi[r] = from_f32<__bf16>(v);
-          lo[r] = from_f32<__bf16>(v - to_f32(hi[r]));
+          const bool on = first + (tb != sb ? 0 : r) <= 0 && nn[r] == nt;
+          v[r] = on ? a.scale * p[r] * __builtin_amdgcn_exp2f(dt - ds[r]) : 0.f;
         }
         const int at = weight_at(t, 2 * sb + (g >> 1)) + (g & 1) * 8;
-        *reinterpret_cast<b4 *>(lp + at) = hi;
-        *reinterpret_cast<b4 *>(lpl + at) = lo;
-      }
+        uint2 w;
+        w.x = take2(v[0], v[1], __bf16());
+        w.y = take2(v[2], v[3], __bf16());
+        *reinterpret_cast<uint2 *>(lp + at) = w;
+        w.x = pack2<__bf16>(v[0], v[1]);
+        w.y = pack2<__bf16>(v[2], v[3]);
+        *reinterpret_cast<uint2 *>(lpl + at) = w;
+      };
+      weights(wave);
+      weights(wave + 4);
+      if (wave < 2)
+        weights(wave + 8);
+      else if (more && wave - 2 == ((t0 / kBlock) & 1))
+        make_table(gt, a.scale, tab.carry, lane, tables[buf ^ 1]);
       // what the state contributes
 #pragma unroll
       for (int tb = 0; tb < 4; ++tb)
@@ -456,22 +508,23 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
       }
 #pragma unroll
       for (int j = 0; j < KT; ++j) {
-        v8 sh[NT], sl[NT];
+        u4 sh[NT], sl[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float v = F16 ? S[2 * j + (e >> 2)][n][e & 3] * sf[n] : S[2 * j + (e >> 2)][n][e & 3];
-            sh[n][e] = from_f32<T>(v);
-            sl[n][e] = from_f32<T>(v - to_f32(sh[n][e]));
+          for (int e = 0; e < 8; e += 2) {
+            float x = S[2 * j + (e >> 2)][n][e & 3], y = S[2 * j + (e >> 2)][n][(e & 3) + 1];
+            if constexpr (F16) x *= sf[n], y *= sf[n];
+            sh[n][e / 2] = take2(x, y, T());
+            sl[n][e / 2] = pack2<T>(x, y);
           }
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb) {
-          const v8 fq = row_operand<T, KT>(lq, 16 * tb + c, j, lane);
+          const v8 fq = row_operand<T, KT>(lq, at_row, tb, j);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            O[tb][n] = Half<T>::mfma16(sh[n], fq, O[tb][n]);
-            O[tb][n] = Half<T>::mfma16(sl[n], fq, O[tb][n]);
+            O[tb][n] = Half<T>::mfma16(__builtin_bit_cast(v8, sh[n]), fq, O[tb][n]);
+            O[tb][n] = Half<T>::mfma16(__builtin_bit_cast(v8, sl[n]), fq, O[tb][n]);
           }
         }
       }
@@ -490,8 +543,8 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
         }
       }
     }
-    if (more && wave == ((t0 / kBlock) & 3)) make_table(gt, a.scale, tab.carry, lane, tables[buf ^ 1]);  // the next block's, by each wave in turn
     if constexpr (!OUT) {
+      if (more && wave == ((t0 / kBlock) & 3)) make_table(gt, a.scale, tab.carry, lane, tables[buf ^ 1]);  // the next block's, by each wave in turn
       G += tab.sum;
       resets += tab.resets;
     }
@@ -543,21 +596,19 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
           }
         }
         const int t = t0 + 16 * tb + c;
-        if (t < t_hi) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n) {
+          const v4f o = O[tb][n];
+          if constexpr (WIDE) {
+            typedef unsigned u2 __attribute__((ext_vector_type(2)));
+            const u2 w = {pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+            __builtin_amdgcn_raw_buffer_store_b64(w, buffer_over(po + (size_t)t0 * a.ldo, 0x7fffffff), t < t_hi ? oo[n] : OFF,
+                                                  (int)(16 * tb * a.ldo * 2), 0);
+          } else if (t < t_hi) {
             const int col = col0 + 16 * n + 4 * g;
-            typename Half<T>::v4 o;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(O[tb][n][r]);
-            T *to = po + (size_t)t * a.ldo + col;
-            if (col + 4 <= a.dv) {
-              __builtin_memcpy(to, &o, 8);
-            } else if constexpr (!WIDE) {
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (col + r < a.dv) to[r] = o[r];
-            }
+            for (int r = 0; r < 4; ++r)
+              if (col + r < a.dv) po[(size_t)t * a.ldo + col + r] = from_f32<T>(o[r]);
           }
         }
       }
@@ -565,7 +616,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 
     // the state's update: decay, then k (weighted v)^T
     constexpr int VP = F16 ? 2 : 3;
-    v8 wv[VP][2][NT];
+    u4 wv[VP][2][NT];
     float back[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -590,19 +641,18 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float v = F16 ? x[kb][e] * up : x[kb][e];
+        for (int e = 0; e < 8; e += 2) {
+          float v0 = x[kb][e], v1 = x[kb][e + 1];
+          if constexpr (F16) v0 *= up, v1 *= up;
 #pragma unroll
-          for (int p = 0; p < VP; ++p) {
-            wv[p][kb][n][e] = from_f32<T>(v);
-            v -= to_f32(wv[p][kb][n][e]);
-          }
+          for (int p = 0; p + 1 < VP; ++p) wv[p][kb][n][e / 2] = take2(v0, v1, T());
+          wv[VP - 1][kb][n][e / 2] = pack2<T>(v0, v1);
         }
     }
     const float dec = tab.dec;
 #pragma unroll
     for (int i = 0; i < 2 * KT; ++i) {
-      const v8 k0 = column_operand<T, KT>(lk, 0, i, lane), k1 = column_operand<T, KT>(lk, 1, i, lane);
+      const v8 k0 = column_operand<T, KT>(lks, at_column, 0, i), k1 = column_operand<T, KT>(lks, at_column, 1, i);
       v4f u[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -612,8 +662,8 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
       for (int p = VP - 1; p >= 0; --p)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          u[n] = Half<T>::mfma16(k0, wv[p][0][n], u[n]);
-          u[n] = Half<T>::mfma16(k1, wv[p][1][n], u[n]);
+          u[n] = Half<T>::mfma16(k0, __builtin_bit_cast(v8, wv[p][0][n]), u[n]);
+          u[n] = Half<T>::mfma16(k1, __builtin_bit_cast(v8, wv[p][1][n]), u[n]);
         }
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -717,7 +767,7 @@ int run_prefill(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t s
 // Rows that the direct-to-LDS loads can take: every row and head starts on 16 bytes, 64 rows lie within 2^31 bytes.
 bool wide_rows(const LinAttnArgs &a) {
   const long long most = 1LL << 23;
-  return aligned(a.q, 16) && aligned(a.k, 16) && aligned(a.v, 16) && a.ldq % 8 == 0 && a.ldk % 8 == 0 && a.ldv % 8 == 0 && a.dk % 8 == 0 &&
+  return aligned(a.q, 16) && aligned(a.k, 16) && aligned(a.v, 16) && aligned(a.out, 8) && a.ldo % 4 == 0 && a.ldo < most && a.ldq % 8 == 0 && a.ldk % 8 == 0 && a.ldv % 8 == 0 && a.dk % 8 == 0 &&
          a.dv % 8 == 0 && a.ldq < most && a.ldk < most && a.ldv < most;
 }
 
