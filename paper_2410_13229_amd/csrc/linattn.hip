@@ -29,44 +29,74 @@ constexpr float LOG2E = 1.44269504088896340736f;
 // a = exp(min(g, 0)); NaN stays NaN, -inf gives 0
 __device__ __forceinline__ float decay_of(float g) { return __builtin_amdgcn_exp2f((g > 0.f ? 0.f : g) * LOG2E); }
 
-// Token by token: a workgroup keeps 16 columns of one head's state in registers, 16 threads with 16 rows each per
-// column; every token's products with q are added over those threads.
-template <typename T>
-__global__ __launch_bounds__(256) void linattn_tokens_kernel(LinAttnArgs a) {
-  __shared__ float sq[256], sk[256], red[16][17];
-  const int tid = threadIdx.x, c = tid & 15, r0 = (tid >> 4) * 16;
-  const int h = blockIdx.y, b = blockIdx.z, col = blockIdx.x * 16 + c, hk = h / (a.Hv / a.Hk);
-  const int len = a.lens ? min(max(a.lens[b], 0), a.L) : a.L;
-  float *st = a.state ? a.state + ((size_t)b * a.Hv + h) * a.dk * a.dv : nullptr;
-  float S[16];
+// One token: bound by reading and writing the state (64 sequences, 80 heads of 128 x 64: 336 MB, at the rate a copy reaches 66 us).
+// A workgroup takes 64 columns of one head's state, rows in turn over its threads, V columns a thread (4: 16-byte accesses along
+// the rows); all of its reads leave before anything is waited for.  Row sums of q S are added over the lanes, then over the
+// waves, in a fixed order.
+template <typename T, int V, int RPT>
+__global__ __launch_bounds__(256) void linattn_step_kernel(LinAttnArgs a) {
+  constexpr int LPR = 64 / V, RPP = 256 / LPR;  // lanes along a row, rows at a time
+  typedef float vf __attribute__((ext_vector_type(V)));
+  __shared__ float sq[RPT * RPP], sk[RPT * RPP], red[4][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r0 = tid / LPR, cc = tid % LPR * V;
+  const int h = blockIdx.y, b = blockIdx.z, col = blockIdx.x * 64 + cc, hk = h / (a.Hv / a.Hk);
+  float *st = a.state + ((size_t)b * a.Hv + h) * a.dk * a.dv;
+  const bool in = col < a.dv;  // V = 4: dv is a multiple of 4
+  vf S[RPT];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) S[i] = st && r0 + i < a.dk && col < a.dv ? st[(size_t)(r0 + i) * a.dv + col] : 0.f;
-  for (int t = 0; t < len; ++t) {
-    const size_t row = (size_t)b * a.L + t;
-    sq[tid] = tid < a.dk ? to_f32(static_cast<const T *>(a.q)[row * a.ldq + (size_t)hk * a.dk + tid]) : 0.f;
-    sk[tid] = tid < a.dk ? to_f32(static_cast<const T *>(a.k)[row * a.ldk + (size_t)hk * a.dk + tid]) : 0.f;
-    __syncthreads();
-    const float vv = col < a.dv ? to_f32(static_cast<const T *>(a.v)[row * a.ldv + (size_t)h * a.dv + col]) : 0.f;
-    const float al = a.g ? decay_of(a.ldg ? a.g[row * a.ldg + h] : a.g[h]) : 1.f;
-    float o = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      S[i] = fmaf(al, S[i], sk[r0 + i] * vv);
-      o = fmaf(sq[r0 + i], S[i], o);
-    }
-    red[tid >> 4][c] = o;
-    __syncthreads();
-    if (tid < 16 && col < a.dv) {
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s += red[i][c];
-      static_cast<T *>(a.out)[row * a.ldo + (size_t)h * a.dv + col] = from_f32<T>(a.scale * s);
-    }
+  for (int i = 0; i < RPT; ++i) {
+    const int row = r0 + i * RPP;
+    S[i] = vf(0.f);
+    if (in && row < a.dk) S[i] = *reinterpret_cast<const vf *>(st + (size_t)row * a.dv + col);
   }
-  if (st)
+  const T *q = static_cast<const T *>(a.q) + (size_t)b * a.ldq + (size_t)hk * a.dk, *k = static_cast<const T *>(a.k) + (size_t)b * a.ldk + (size_t)hk * a.dk;
+  for (int i = tid; i < RPT * RPP; i += 256) {
+    sq[i] = i < a.dk ? to_f32(q[i]) : 0.f;
+    sk[i] = i < a.dk ? to_f32(k[i]) : 0.f;
+  }
+  float v[V], o[V];
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (r0 + i < a.dk && col < a.dv) st[(size_t)(r0 + i) * a.dv + col] = S[i];
+  for (int e = 0; e < V; ++e) {
+    v[e] = in ? to_f32(static_cast<const T *>(a.v)[(size_t)b * a.ldv + (size_t)h * a.dv + col + e]) : 0.f;
+    o[e] = 0.f;
+  }
+  const float al = a.g ? decay_of(a.ldg ? a.g[(size_t)b * a.ldg + h] : a.g[h]) : 1.f;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < RPT; ++i) {
+    const int row = r0 + i * RPP;
+    const float kk = sk[row], qq = sq[row];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      S[i][e] = fmaf(al, S[i][e], kk * v[e]);
+      o[e] = fmaf(qq, S[i][e], o[e]);
+    }
+    if (in && row < a.dk) *reinterpret_cast<vf *>(st + (size_t)row * a.dv + col) = S[i];
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+#pragma unroll
+    for (int m = LPR; m < 64; m *= 2) o[e] += __shfl_xor(o[e], m);
+    if (lane < LPR) red[wave][cc + e] = o[e];
+  }
+  __syncthreads();
+  if (tid < 64 && blockIdx.x * 64 + tid < a.dv)
+    static_cast<T *>(a.out)[(size_t)b * a.ldo + (size_t)h * a.dv + blockIdx.x * 64 + tid] =
+        from_f32<T>(a.scale * (red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid]));
+}
+
+template <typename T, int V>
+int run_step(const LinAttnArgs &a, hipStream_t st) {
+  constexpr int RPP = 4 * V;
+  const dim3 grid((a.dv + 63) / 64, a.Hv, a.Bt);
+  if (a.dk <= 4 * RPP)
+    hipLaunchKernelGGL((linattn_step_kernel<T, V, 4>), grid, dim3(256), 0, st, a);
+  else if (a.dk <= (V == 4 ? 8 : 32) * RPP)
+    hipLaunchKernelGGL((linattn_step_kernel<T, V, V == 4 ? 8 : 32>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((linattn_step_kernel<T, V, V == 4 ? 16 : 64>), grid, dim3(256), 0, st, a);
+  QUAMBA_LAUNCH_CHECK();
+  return QUAMBA_OK;
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -827,13 +857,9 @@ int quamba_linattn_step(int type, const void *q, int ldq, const void *k, int ldk
   const int rc = check("linattn_step", type, a);
   if (rc != QUAMBA_OK || Bt == 0) return rc;
   if (!state) return fail(QUAMBA_EINVAL, "linattn_step: state is required");
-  const dim3 grid((dv + 15) / 16, Hv, Bt);
-  if (type == QUAMBA_TYPE_F16)
-    hipLaunchKernelGGL(linattn_tokens_kernel<_Float16>, grid, dim3(256), 0, as_stream(stream), a);
-  else
-    hipLaunchKernelGGL(linattn_tokens_kernel<__bf16>, grid, dim3(256), 0, as_stream(stream), a);
-  QUAMBA_LAUNCH_CHECK();
-  return QUAMBA_OK;
+  hipStream_t st = as_stream(stream);
+  if (type == QUAMBA_TYPE_F16) return dv % 4 == 0 ? run_step<_Float16, 4>(a, st) : run_step<_Float16, 1>(a, st);
+  return dv % 4 == 0 ? run_step<__bf16, 4>(a, st) : run_step<__bf16, 1>(a, st);
 }
 
 }  // extern "C"
