@@ -582,8 +582,9 @@ int quamba_model_generate(const quamba_model *model, const int32_t *first_tokens
  *   fp32, rounded once to the output.  residual may be `out` itself (ldr = ldo), the residual stream updated in place; otherwise
  *   out must not overlap any input.  A row's result is the same whatever other rows hold, but may differ in the last bits
  *   between calls of different M (another order of the sums).
- *   ws (16-byte aligned, may be NULL): room for the partial sums of a K split over the grid; with less than
- *   quamba_linear_workspace_bytes K is split less or not at all, which only costs time.  M = 0 is allowed and does nothing. */
+ *   ws (256-byte aligned, may be NULL): quamba_linear_workspace_bytes bytes make room for copies of x and W with rows on 16
+ *   bytes, which a product of more than 16 rows is computed from if theirs do not start there (pointer, stride and K); without
+ *   them such a product takes about twice the time.  Not used otherwise.  M = 0 is allowed and does nothing. */
 #define QUAMBA_TYPE_F16 1
 #define QUAMBA_TYPE_BF16 2
 #define QUAMBA_TYPE_F32 3
@@ -674,7 +675,7 @@ int quamba_probe_rate(int probe, int waves_per_simd, int iters, double *instr_pe
  *                                      the GPU is shared; 3 = all blocks in one launch whose first input never
  *                                      arrives (its waits run out, about 0.3 s a step); 0 = default (all blocks in one
  *                                      launch where served)
- *   quamba_debug_set_linear_variant(v) v >= 0 forces kernel configuration v (0..9) of quamba_linear where the shape
+ *   quamba_debug_set_linear_variant(v) v >= 0 forces kernel configuration v (0..11) of quamba_linear where the shape
  *                                      allows it; -1 = chosen per shape (default); sums are added in another order
  * Host-only queries of what is chosen for a shape with the full workspace, for tests of the rules:
  *   quamba_debug_gemm_kind(M, N, K)    configuration of an int8 GEMM as quamba_debug_set_gemm_variant counts

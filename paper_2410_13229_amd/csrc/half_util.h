@@ -39,6 +39,12 @@ __device__ __forceinline__ T from_f32(float v) {
   return static_cast<T>(v);
 }
 
+// 16 bytes a lane from the buffer's offset off (lane) + soff (wave) to consecutive LDS from `to` on; zeros where off is past the
+// buffer's end (the test looks at off alone)
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t buffer, int off, int soff, char *to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (void __attribute__((address_space(3))) *)to, 16, off, soff, 0, 0);
+}
+
 // Eight consecutive elements of a row from element k on, zeros past K.  A 16-byte load at any element's address.
 template <typename T>
 __device__ __forceinline__ typename Half<T>::v8 row8(const T *row, int k, int K) {

@@ -286,11 +286,6 @@ __device__ __forceinline__ float max_over_groups(float m) {
 
 __device__ __forceinline__ int seq_len(const LinAttnArgs &a, int b) { return a.lens ? min(max(a.lens[b], 0), a.L) : a.L; }
 
-// 16 bytes a lane from base + off (lane) + soff (wave) to consecutive LDS from `to` on; zeros where off is past the buffer
-__device__ __forceinline__ void load_to_lds(const void *base, int off, int soff, char *to) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_over(base, 0x7fffffff), (void __attribute__((address_space(3))) *)to, 16, off, soff, 0, 0);
-}
-
 // Two fp32 values as one word of 16-bit ones, rounded to nearest
 template <typename T>
 __device__ __forceinline__ unsigned pack2(float a, float b) {
@@ -391,7 +386,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
       const int n = t_hi - t0;  // rows that count
       if constexpr (WIDE) {
         const int off = n >= kBlock || tile_row(i) < n ? o[i % PH] : OFF;
-        load_to_lds(p + (size_t)t0 * ld, off, (int)((i / PH) * (PH * 4 * RPL) * ld * 2), tile + ((i / PH) * PH * 4 + (i % PH) * 4 + wave) * 1024);
+        load_to_lds(buffer_over(p + (size_t)t0 * ld, 0x7fffffff), off, (int)((i / PH) * (PH * 4 * RPL) * ld * 2), tile + ((i / PH) * PH * 4 + (i % PH) * 4 + wave) * 1024);
       } else {
         r[i] = tile_row(i) < n ? row8(p + (size_t)(t0 + tile_row(i)) * ld, tile_chunk(i) * 8, a.dk) : zero;
       }
@@ -402,7 +397,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
     for (int i = 0; i < NLV; ++i) {
       const int n = t_hi - t0, row = v_row + RPLV * i;
       if constexpr (WIDE)
-        load_to_lds(pv + (size_t)t0 * a.ldv, n >= kBlock || row < n ? ov : OFF, (int)(RPLV * i * a.ldv * 2), lv + i * 1024);
+        load_to_lds(buffer_over(pv + (size_t)t0 * a.ldv, 0x7fffffff), n >= kBlock || row < n ? ov : OFF, (int)(RPLV * i * a.ldv * 2), lv + i * 1024);
       else
         rv[i] = row < n ? row8(pv + (size_t)(t0 + row) * a.ldv, col0 + v_chunk * 8, a.dv) : zero;
     }

@@ -8,6 +8,7 @@
 #include <climits>
 
 #include "common.h"
+#include "device_util.h"
 #include "half_util.h"
 
 namespace quamba {
@@ -21,7 +22,6 @@ struct LinearEpi {
   void *out;          // [M, ldo]
   long long ldr, ldo;
   int act;
-  bool wide;  // residual and output rows start on 16 bytes
 };
 
 // The activation is evaluated in fp32.  exp2 of a large positive argument is infinite and its reciprocal 0, so the
@@ -47,15 +47,23 @@ __device__ __forceinline__ float activate(float v, int act) {
   }
 }
 
+// One output whose bias and residual are asked for before its sum is there: at a few rows their latency is what is left to save.
+struct Single {
+  float bias = 0.f, res = 0.f;
+  bool on = false;
+};
 template <typename O>
-__device__ __forceinline__ void emit1(const LinearEpi &e, int gm, int gn, float v) {
-  if (e.bias) v += e.bias[gn];
-  v = activate(v, e.act);
-  if (e.res) v += to_f32(static_cast<const O *>(e.res)[(size_t)gm * e.ldr + gn]);
-  static_cast<O *>(e.out)[(size_t)gm * e.ldo + gn] = from_f32<O>(v);
+__device__ __forceinline__ Single ask1(const LinearEpi &e, int gm, int gn, int M, int N) {
+  Single s;
+  s.on = gm < M && gn < N;
+  if (s.on && e.bias) s.bias = e.bias[gn];
+  if (s.on && e.res) s.res = to_f32(static_cast<const O *>(e.res)[(size_t)gm * e.ldr + gn]);
+  return s;
 }
-
-__device__ __forceinline__ v4f zero4() { return v4f{0.f, 0.f, 0.f, 0.f}; }
+template <typename O>
+__device__ __forceinline__ void put1(const LinearEpi &e, const Single &s, int gm, int gn, float v) {
+  if (s.on) static_cast<O *>(e.out)[(size_t)gm * e.ldo + gn] = from_f32<O>(activate(v + s.bias, e.act) + s.res);
+}
 
 // Byte offset of 16-byte chunk `chunk` of tile row `row` for rows of BKB bytes: any 16 consecutive rows read at one
 // logical chunk hit 16 different bank groups (with 64-byte rows four rows span the 64 banks, with 128-byte rows two).
@@ -63,70 +71,89 @@ template <int BKB>
 __device__ __forceinline__ int swz(int row, int chunk) {
   if constexpr (BKB == 64) return row * 64 + ((chunk ^ ((row >> 2) & 3)) << 4);
   else if constexpr (BKB == 128) return row * 128 + ((chunk ^ ((row >> 1) & 7)) << 4);
-  else return row * 256 + ((chunk ^ (row & 15)) << 4);
+  else return row * BKB + ((chunk ^ (row & 15)) << 4);
 }
 
 // A wave's TM x TN tiles of 32 x 32 sums: register r of lane l in tile (i, j) is column n_base + 32 i + 8 (r / 4) + 4 (l / 32)
 // + r % 4 of row m_base + 32 j + l % 32.  A band of 32 rows and up to 64 columns at a time goes through a region of LDS that
 // only this wave uses (fp32, rows 16 bytes further apart than they are long), so that bias, residual and output are
-// taken 16 bytes a lane along the rows, and the epilogue's code exists once and not per tile.
+// taken 16 bytes a lane along the rows (global memory takes such accesses at any element's address).  A band's residual is asked
+// for before its sums are laid out; one trip per row after them cost 4 us of a 22 us call.  The activation is a pass of its own
+// over the band: its code exists once.
 constexpr int kBandPitch = 64 * 4 + 16;
 constexpr int kBandBytes = 32 * kBandPitch;
 
 template <typename O>
-__device__ __forceinline__ void store_band(const LinearEpi &e, int m0, int n0, int cols, int lane, int M, int N, const char *band) {
-  constexpr int E = 16 / sizeof(O);  // elements of a 16-byte store
-  const int per_row = cols / E;
-  const int cc = lane % per_row * E, gn = n0 + cc;
-  if (gn >= N) return;
-  const bool whole = e.wide && gn + E <= N;
-  float b[E];
+struct Band {
+  static constexpr int E = 16 / sizeof(O), IT = 32 * 64 / (64 * E);  // elements of a 16-byte access; accesses of a lane (64 columns)
+  typedef O vO __attribute__((ext_vector_type(E)));
+  int m0, n0, per_row, cc, gn, r0, rows;  // the lane's columns cc ..; rows r0, r0 + rows, ...
+  bool whole;
+  float bias[E];
+  vO res[IT];
+
+  __device__ __forceinline__ void ask(const LinearEpi &e, int m, int n, int cols, int lane, int M, int N) {
+    m0 = m, n0 = n, per_row = cols / E, cc = lane % per_row * E, gn = n0 + cc, r0 = lane / per_row, rows = 64 / per_row;
+    whole = gn + E <= N;
 #pragma unroll
-  for (int i = 0; i < E; ++i) b[i] = e.bias && gn + i < N ? e.bias[gn + i] : 0.f;
-#pragma unroll 1
-  for (int r = lane / per_row; r < 32; r += 64 / per_row) {
-    const int gm = m0 + r;
-    if (gm >= M) return;
-    float v[E];
+    for (int i = 0; i < E; ++i) bias[i] = e.bias && gn + i < N ? e.bias[gn + i] : 0.f;
+    if (e.res && whole) {
 #pragma unroll
-    for (int i = 0; i < E; i += 4) {
-      const v4f t = *reinterpret_cast<const v4f *>(band + r * kBandPitch + (cc + i) * 4);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) v[i + c] = t[c] + b[i + c];
-    }
-    if (e.act != QUAMBA_ACT_NONE) {
-#pragma unroll
-      for (int i = 0; i < E; ++i) v[i] = activate(v[i], e.act);
-    }
-    const O *res = static_cast<const O *>(e.res) + (size_t)gm * e.ldr + gn;
-    O *out = static_cast<O *>(e.out) + (size_t)gm * e.ldo + gn;
-    typedef O vO __attribute__((ext_vector_type(E)));
-    if (whole) {
-      if (e.res) {
-        const vO t = *reinterpret_cast<const vO *>(res);
-#pragma unroll
-        for (int i = 0; i < E; ++i) v[i] += to_f32(t[i]);
+      for (int it = 0; it < IT; ++it) {
+        const int r = r0 + it * rows;
+        if (r < 32 && m0 + r < M) __builtin_memcpy(&res[it], static_cast<const O *>(e.res) + (size_t)(m0 + r) * e.ldr + gn, 16);
       }
-      vO t;
-#pragma unroll
-      for (int i = 0; i < E; ++i) t[i] = from_f32<O>(v[i]);
-      *reinterpret_cast<vO *>(out) = t;
-    } else {
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (gn + i < N) out[i] = from_f32<O>(e.res ? v[i] + to_f32(res[i]) : v[i]);
     }
   }
-}
+  __device__ __forceinline__ void put(const LinearEpi &e, int M, int N, char *band) const {
+    if (e.act != QUAMBA_ACT_NONE) {
+#pragma unroll 1
+      for (int r = r0; r < 32; r += rows)
+#pragma unroll
+        for (int i = 0; i < E; i += 4) {
+          v4f *p = reinterpret_cast<v4f *>(band + r * kBandPitch + (cc + i) * 4);
+          v4f t = *p;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) t[c] = activate(t[c] + bias[i + c], e.act);
+          *p = t;
+        }
+    }
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+      const int r = r0 + it * rows, gm = m0 + r;
+      if (r >= 32 || gm >= M || gn >= N) continue;
+      float v[E];
+#pragma unroll
+      for (int i = 0; i < E; i += 4) {
+        const v4f t = *reinterpret_cast<const v4f *>(band + r * kBandPitch + (cc + i) * 4);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[i + c] = e.act != QUAMBA_ACT_NONE ? t[c] : t[c] + bias[i + c];
+      }
+      O *out = static_cast<O *>(e.out) + (size_t)gm * e.ldo + gn;
+      if (whole) {
+        vO t;
+#pragma unroll
+        for (int i = 0; i < E; ++i) t[i] = from_f32<O>(e.res ? v[i] + to_f32(res[it][i]) : v[i]);
+        __builtin_memcpy(out, &t, 16);
+      } else {
+        const O *rp = static_cast<const O *>(e.res) + (size_t)gm * e.ldr + gn;
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+          if (gn + i < N) out[i] = from_f32<O>(e.res ? v[i] + to_f32(rp[i]) : v[i]);
+      }
+    }
+  }
+};
 
-// `partial`: raw sums to partial[M, N] instead (K split over the grid).
 template <typename O, int TM, int TN>
 __device__ __forceinline__ void store_wave(const v16f (&acc)[TN][TM], int m_base, int n_base, int lane, int M, int N, const LinearEpi &e,
-                                           float *partial, char *band) {
+                                           char *band) {
   constexpr int PER = (TN + 1) / 2;  // bands of columns
 #pragma unroll 1
   for (int step = 0; step < TM * PER; ++step) {
     const int j = step / PER, i0 = step % PER * 2;
+    Band<O> b;
+    b.ask(e, m_base + 32 * j, n_base + 32 * i0, i0 + 1 < TN ? 64 : 32, lane, M, N);
 #pragma unroll
     for (int s = 0; s < TM * PER; ++s)
       if (s == step) {
@@ -137,13 +164,7 @@ __device__ __forceinline__ void store_wave(const v16f (&acc)[TN][TM], int m_base
             *reinterpret_cast<v4f *>(band + (lane & 31) * kBandPitch + ((i & 1) * 32 + 8 * g + 4 * (lane >> 5)) * 4) =
                 v4f{acc[i][s / PER][4 * g], acc[i][s / PER][4 * g + 1], acc[i][s / PER][4 * g + 2], acc[i][s / PER][4 * g + 3]};
       }
-    const int cols = i0 + 1 < TN ? 64 : 32;
-    if (partial) {
-      const LinearEpi raw{nullptr, nullptr, partial, 0, N, QUAMBA_ACT_NONE, (N & 3) == 0};
-      store_band<float>(raw, m_base + 32 * j, n_base + 32 * i0, cols, lane, M, N, band);
-    } else {
-      store_band<O>(e, m_base + 32 * j, n_base + 32 * i0, cols, lane, M, N, band);
-    }
+    b.put(e, M, N, band);
   }
 }
 
@@ -157,17 +178,11 @@ __device__ __forceinline__ void tile_of(int wg, int tiles_m, int tiles_n, int *t
   *tn = r / rows;
 }
 
-struct KRange {
-  int slices;      // K slices of one grid.y index
-  float *partial;  // [grid.y, M, N] sums when K is split, else NULL
-};
-
 // Any strides and alignments: K in slices of 32 staged through registers (16-byte loads at element addresses, which
 // global memory serves at whatever lines they touch), two LDS stages, four waves in 2 x 2.
 template <typename T, typename O, int TM, int TN>
 __global__ __launch_bounds__(256) void linear_any_kernel(const T *__restrict__ x, long long ldx, const T *__restrict__ W,
-                                                         long long ldw, int M, int N, int K, LinearEpi epi, int tiles_m, int tiles_n,
-                                                         KRange kr) {
+                                                         long long ldw, int M, int N, int K, LinearEpi epi, int tiles_m, int tiles_n) {
   constexpr int BK = 32, BM = 64 * TM, BN = 64 * TN, STAGE = (BM + BN) * BK * 2;
   constexpr int LDS = 2 * STAGE > 4 * kBandBytes ? 2 * STAGE : 4 * kBandBytes;
   __shared__ __attribute__((aligned(16))) char lds[LDS];
@@ -177,8 +192,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(const T *__restrict__ x
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave & 1, wn = wave >> 1;
   const int row = tid >> 2, ch = tid & 3;
-  const int k_lo = blockIdx.y * kr.slices * BK;
-  const int nk = min((K + BK - 1) / BK - blockIdx.y * kr.slices, kr.slices);
+  const int nk = (K + BK - 1) / BK;
 
   v16f acc[TN][TM];
 #pragma unroll
@@ -196,7 +210,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(const T *__restrict__ x
   for (int i = 0; i < TN; ++i) pw[i] = W + (size_t)min(n0 + 64 * i + row, N - 1) * ldw;
   typename Half<T>::v8 rx[TM], rw[TN];
   auto fetch = [&](int kt) {
-    const int gk = k_lo + kt * BK + ch * 8;
+    const int gk = kt * BK + ch * 8;
 #pragma unroll
     for (int j = 0; j < TM; ++j) rx[j] = row8(px[j], gk, K);
 #pragma unroll
@@ -231,17 +245,13 @@ __global__ __launch_bounds__(256) void linear_any_kernel(const T *__restrict__ x
     if (kt + 1 < nk) park((kt + 1) & 1);
     __syncthreads();
   }
-  store_wave<O, TM, TN>(acc, m0 + wm * TM * 32, n0 + wn * TN * 32, lane, M, N, epi, kr.partial ? kr.partial + (size_t)blockIdx.y * M * N : nullptr,
-                        lds + wave * kBandBytes);
+  store_wave<O, TM, TN>(acc, m0 + wm * TM * 32, n0 + wn * TN * 32, lane, M, N, epi, lds + wave * kBandBytes);
 }
 
-// 16-byte rows: slices travel with the 16-byte direct-to-LDS loads (no staging registers, no LDS write instructions).  A
-// wave-level load writes 64 lanes x 16 bytes at LDS base + 16 lane, 1024 / BKB consecutive tile rows, so the swizzle is applied
-// on the global side: each lane fetches the chunk that belongs in its slot.  Chunks past K are fetched from a
-// block of zeros, rows past M or N repeat the last row (multiplied, never stored).
+// 16-byte rows: slices travel with 16-byte direct-to-LDS buffer loads (no staging registers, no LDS write instructions).  A
+// wave-level load writes 64 lanes x 16 bytes of consecutive LDS, 1024 / BKB tile rows, so the swizzle is applied on the global
+// side: each lane fetches the chunk that belongs in its slot; rows past M or N and chunks past K arrive as zeros.
 // Ring of S stages; KG groups of waves share one tile, group g multiplying the 32-byte sub-slices s with s % KG == g.
-__device__ __attribute__((aligned(16))) const unsigned g_zeros[4] = {0, 0, 0, 0};
-
 // s_waitcnt for "at most n vector loads outstanding, nothing else waited for" (vmcnt in bits 3:0 and 15:14, expcnt 6:4,
 // lgkmcnt 11:8), and with this wave's LDS reads finished as well
 #define QUAMBA_VMCNT(n) (((n) & 0xF) | ((((n) >> 4) & 0x3) << 14) | (0x7 << 4) | (0xF << 8))
@@ -250,9 +260,9 @@ __device__ __attribute__((aligned(16))) const unsigned g_zeros[4] = {0, 0, 0, 0}
 template <typename T, typename O, int BM, int BN, int WGM, int WGN, int S, int BKB, int OCC, int KG>
 __global__ __launch_bounds__(64 * WGM * WGN * KG, OCC) void linear_dma_kernel(const T *__restrict__ x, long long ldx, const T *__restrict__ W,
                                                                               long long ldw, int M, int N, int K, LinearEpi epi, int tiles_m,
-                                                                              int tiles_n, KRange kr) {
+                                                                              int tiles_n) {
   constexpr int NW = WGM * WGN * KG, WM = BM / WGM, WN = BN / WGN, TM = WM / 32, TN = WN / 32;
-  constexpr int RPI = 1024 / BKB, CPR = BKB / 16, ROWS = BM + BN, NJ = ROWS / RPI, NI = (NJ + NW - 1) / NW, STAGE = ROWS * BKB;
+  constexpr int RPI = 1024 / BKB, CPR = BKB / 16, ROWS = BM + BN, NJ = ROWS / RPI, NI = NJ / NW, STAGE = ROWS * BKB;
   constexpr int NSUB = BKB / 32 / KG, BKE = BKB / 2;  // sub-slices of a group; elements of a slice
   static_assert(WM % 32 == 0 && WN % 32 == 0 && BM % RPI == 0 && BN % RPI == 0 && BKB / 32 % KG == 0, "tile");
   static_assert((S - 2) * NI <= 63 && S >= 2 && (S > 2 || (NSUB >= 2 && KG == 1)), "ring");
@@ -262,39 +272,28 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, OCC) void linear_dma_kernel(co
   int tile_m, tile_n;
   tile_of(blockIdx.x, tiles_m, tiles_n, &tile_m, &tile_n);
   const int m0 = tile_m * BM, n0 = tile_n * BN;
-  const int slice_lo = blockIdx.y * kr.slices;
-  const int nk = min((K + BKE - 1) / BKE - slice_lo, kr.slices);
+  const int nk = (K + BKE - 1) / BKE;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kg = wave / (WGM * WGN), wtile = wave % (WGM * WGN), wm = wtile % WGM, wn = wtile / WGM;
 
-  auto load_row = [&](int i) { return min(wave + NW * i, NJ - 1) * RPI + lane / CPR; };  // a short wave repeats the last group
-  auto k_of = [&](int i) {  // first k of this lane's chunk of load i in slice 0; the swizzle's phase follows the row inside its operand
-    const int row = load_row(i), lrow = row < BM ? row : row - BM;
-    return slice_lo * BKE + ((swz<BKB>(lrow, lane % CPR) - lrow * BKB) >> 4) * 8;
-  };
-  const T *src[NI];
-  int dst[NI];
-#pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int row = load_row(i);
-    dst[i] = min(wave + NW * i, NJ - 1) * 1024;
-    src[i] = (row < BM ? x + (size_t)min(m0 + row, M - 1) * ldx : W + (size_t)min(n0 + row - BM, N - 1) * ldw) + k_of(i);
-  }
-  const int ragged = K % BKE ? (K / BKE) - slice_lo : -1;  // the slice that ends past K
+  // Load i of a wave takes tile rows ROWS_I i + row on: the swizzle's phase is the same for all of them, and the first BM / ROWS_I
+  // loads are x's.  A lane's offset reaches past the buffer where its row or (in the last slice) its chunk does not exist.
+  constexpr int ROWS_I = NW * RPI, OFF = (int)0x80000000;
+  static_assert(NJ % NW == 0 && ROWS_I % 16 == 0 && BM % ROWS_I == 0, "loads");
+  const int row = wave * RPI + lane / CPR, chunk = (swz<BKB>(row, lane % CPR) - row * BKB) >> 4;
+  const int ox = row * (int)ldx * 2 + chunk * 16, ow = row * (int)ldw * 2 + chunk * 16;
+  const int step_x = ROWS_I * (int)ldx * 2, step_w = ROWS_I * (int)ldw * 2;
+  auto end_of = [](long long bytes) { return (int)(bytes < 0x7fffffff ? bytes : 0x7fffffff); };
+  const auto bx = buffer_over(x + (size_t)m0 * ldx, end_of((long long)(M - m0) * ldx * 2));
+  const auto bw = buffer_over(W + (size_t)n0 * ldw, end_of((long long)(N - n0) * ldw * 2));
   auto issue = [&](int stage, int slice) {
-    if (slice == ragged) {
+    const bool off = slice * BKE + chunk * 8 >= K;
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const void *p = k_of(i) + slice * BKE < K ? static_cast<const void *>(src[i] + slice * BKE) : static_cast<const void *>(g_zeros);
-        __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)p,
-                                         (void __attribute__((address_space(3))) *)(ring + stage * STAGE + dst[i]), 16, 0, 0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-        __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)(src[i] + slice * BKE),
-                                         (void __attribute__((address_space(3))) *)(ring + stage * STAGE + dst[i]), 16, 0, 0);
+    for (int i = 0; i < NI; ++i) {
+      const bool is_x = i * ROWS_I < BM;
+      const int at = is_x ? ox + i * step_x : ow + (i - BM / ROWS_I) * step_w;
+      load_to_lds(is_x ? bx : bw, off ? OFF : at, slice * BKB, ring + stage * STAGE + (wave + NW * i) * 1024);
     }
   };
 
@@ -307,13 +306,18 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, OCC) void linear_dma_kernel(co
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
   typedef typename Half<T>::v8 v8;
+  // the lane's offset of the group's first chunk in row lane % 32: another sub-slice is an exclusive-or away (as the swizzle's own
+  // exchange of chunks is), 32 rows a constant.  Opaque per slice, or the sums are hoisted and take the registers of the tile
+  const int at_lane = swz<BKB>(lane & 31, kg * 2 + (lane >> 5));
   auto frags = [&](int stage, int sub, v8 (&fx)[TM], v8 (&fw)[TN]) {
-    const char *lx = ring + stage * STAGE, *lw = lx + BM * BKB;
-    const int chunk = (sub * KG + kg) * 2 + (lane >> 5);
+    int at = at_lane;
+    if constexpr (TM * TN > 8) asm volatile("" : "+v"(at));
+    const char *lx = ring + stage * STAGE + wm * WM * BKB + (at ^ (sub * KG * 32));
+    const char *lw = ring + stage * STAGE + (BM + wn * WN) * BKB + (at ^ (sub * KG * 32));
 #pragma unroll
-    for (int j = 0; j < TM; ++j) fx[j] = *reinterpret_cast<const v8 *>(lx + swz<BKB>(wm * WM + j * 32 + (lane & 31), chunk));
+    for (int j = 0; j < TM; ++j) fx[j] = *reinterpret_cast<const v8 *>(lx + j * 32 * BKB);
 #pragma unroll
-    for (int i = 0; i < TN; ++i) fw[i] = *reinterpret_cast<const v8 *>(lw + swz<BKB>(wn * WN + i * 32 + (lane & 31), chunk));
+    for (int i = 0; i < TN; ++i) fw[i] = *reinterpret_cast<const v8 *>(lw + i * 32 * BKB);
   };
   auto mma = [&](const v8 (&fx)[TM], const v8 (&fw)[TN]) {
 #pragma unroll
@@ -416,90 +420,146 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, OCC) void linear_dma_kernel(co
     }
     band = ring + wtile * PART;
   }
-  store_wave<O, TM, TN>(acc, m0 + wm * WM, n0 + wn * WN, lane, M, N, epi, kr.partial ? kr.partial + (size_t)blockIdx.y * M * N : nullptr, band);
+  store_wave<O, TM, TN>(acc, m0 + wm * WM, n0 + wn * WN, lane, M, N, epi, band);
 }
 #undef QUAMBA_VMCNT
 #undef QUAMBA_VMCNT_LGKM0
 
-// Few rows: the job is to read W once.  A workgroup owns 16 columns, its NW waves split K in contiguous ranges, and the
-// fragments go straight from memory to the matrix unit: 16 rows of W against MT x 16 rows of x (rows past M repeat the
+// Up to 16 rows of W and x that do not start on 16 bytes: a workgroup owns 16 columns, its 8 waves split K in contiguous
+// ranges, and the fragments go straight from memory to the matrix unit, 16 rows of W against 16 of x (rows past M repeat the
 // last one; their results are columns that nobody stores).  The waves' sums are added in LDS.
-template <typename T, typename O, int MT, int NW>
-__global__ __launch_bounds__(64 * NW) void linear_rows_kernel(const T *__restrict__ x, long long ldx, const T *__restrict__ W, long long ldw,
-                                                              int M, int N, int K, LinearEpi epi) {
-  constexpr int U = MT == 1 ? 8 : (MT == 2 ? 6 : 4);  // pieces of 32 k in flight
-  __shared__ float part[NW][MT * 16][17];
+template <typename T, typename O>
+__global__ __launch_bounds__(512) void linear_rows_kernel(const T *__restrict__ x, long long ldx, const T *__restrict__ W, long long ldw, int M,
+                                                          int N, int K, LinearEpi epi) {
+  constexpr int U = 8, NW = 8;  // pieces of 32 k in flight; waves
+  __shared__ float part[NW][16][17];
   typedef typename Half<T>::v8 v8;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, c8 = (lane >> 4) * 8;
   const int n0 = blockIdx.x * 16;
   const int pieces = (K + 31) / 32, per = (pieces + NW - 1) / NW, lo = wave * per, hi = min(pieces, lo + per);
-  const T *pw = W + (size_t)min(n0 + r, N - 1) * ldw;
-  const T *px[MT];
-#pragma unroll
-  for (int j = 0; j < MT; ++j) px[j] = x + (size_t)min(j * 16 + r, M - 1) * ldx;
-  v4f acc[MT];
-#pragma unroll
-  for (int j = 0; j < MT; ++j) acc[j] = zero4();
+  const T *pw = W + (size_t)min(n0 + r, N - 1) * ldw, *px = x + (size_t)min(r, M - 1) * ldx;
+  v4f acc = {0.f, 0.f, 0.f, 0.f};
+  const int gm = threadIdx.x >> 4, gn = n0 + (threadIdx.x & 15);
+  Single one;
+  if (threadIdx.x < 256) one = ask1<O>(epi, gm, gn, M, N);
   for (int p = lo; p < hi; p += U) {
-    v8 fw[U], fx[U][MT];
+    v8 fw[U], fx[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) fw[u] = row8(pw, p + u < hi ? (p + u) * 32 + c8 : K, K);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) fx[u] = row8(px, p + u < hi ? (p + u) * 32 + c8 : K, K);
 #pragma unroll
-      for (int j = 0; j < MT; ++j) fx[u][j] = row8(px[j], p + u < hi ? (p + u) * 32 + c8 : K, K);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int j = 0; j < MT; ++j) acc[j] = Half<T>::mfma16(fw[u], fx[u][j], acc[j]);
+    for (int u = 0; u < U; ++u) acc = Half<T>::mfma16(fw[u], fx[u], acc);
   }
 #pragma unroll
-  for (int j = 0; j < MT; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) part[wave][j * 16 + r][(lane >> 4) * 4 + e] = acc[j][e];
+  for (int e = 0; e < 4; ++e) part[wave][r][(lane >> 4) * 4 + e] = acc[e];
   __syncthreads();
-  for (int i = threadIdx.x; i < MT * 256; i += 64 * NW) {
-    const int gm = i >> 4, gn = n0 + (i & 15);
-    if (gm >= M || gn >= N) continue;
+  if (threadIdx.x < 256) {
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) v += part[w][gm][i & 15];
-    emit1<O>(epi, gm, gn, v);
+    for (int w = 0; w < NW; ++w) v += part[w][gm][threadIdx.x & 15];
+    put1<O>(epi, one, gm, gn, v);
   }
 }
 
-// Sums of a K split added in order, then the epilogue.
-template <typename O>
-__global__ __launch_bounds__(256) void linear_join_kernel(const float *__restrict__ partial, int splits, int M, int N, LinearEpi epi) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, n = (size_t)M * N;
-  if (i >= n) return;
-  float v = 0.f;
-  for (int s = 0; s < splits; ++s) v += partial[s * n + i];
-  emit1<O>(epi, (int)(i / N), (int)(i % N), v);
+// One to four rows: the job is to read W once, at the rate of a copy.  LANES lanes split K of four adjacent columns in 16-byte
+// pieces (64 lanes: 1 KB of a row of W at a time), products and sums in fp32 on the vector unit (at 4 rows half as long as the
+// reading), then over lanes and waves in a fixed order.
+template <typename T, typename O, int MR, int LANES>
+__global__ __launch_bounds__(256) void linear_vec_kernel(const T *__restrict__ x, long long ldx, const T *__restrict__ W, long long ldw, int M,
+                                                         int N, int K, LinearEpi epi) {
+  constexpr int U = MR == 4 ? 1 : 2, GROUPS = 256 / LANES;  // pieces in flight; column groups of a workgroup
+  __shared__ float part[4][MR * 4];
+  typedef typename Half<T>::v8 v8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int group = LANES == 64 ? wave : 0, at = LANES == 64 ? lane : (int)threadIdx.x;
+  const int n0 = (blockIdx.x * GROUPS + group) * 4;
+  const T *pw[4], *px[MR];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) pw[j] = W + (size_t)min(n0 + j, N - 1) * ldw;
+#pragma unroll
+  for (int m = 0; m < MR; ++m) px[m] = x + (size_t)min(m, M - 1) * ldx;
+  float acc[MR][4];
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[m][j] = 0.f;
+  const int mine = LANES == 64 ? lane : (int)threadIdx.x, gm = mine >> 2, gn = n0 + (mine & 3);
+  Single one;
+  if (mine < MR * 4) one = ask1<O>(epi, gm, gn, M, N);
+  for (int k = at * 8; k < K; k += LANES * 8 * U) {
+    v8 w[U][4], v[U][MR];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[u][j] = row8(pw[j], k + u * LANES * 8, K);
+#pragma unroll
+      for (int m = 0; m < MR; ++m) v[u][m] = row8(px[m], k + u * LANES * 8, K);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[m][j] = fmaf(to_f32(v[u][m][e]), to_f32(w[u][j][e]), acc[m][j]);
+  }
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v = acc[m][j];
+#pragma unroll
+      for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+      if (lane == 0) part[wave][m * 4 + j] = v;
+    }
+  __syncthreads();
+  if (mine < MR * 4)
+    put1<O>(epi, one, gm, gn, LANES == 64 ? part[wave][mine] : part[0][mine] + part[1][mine] + part[2][mine] + part[3][mine]);
+}
+
+// Rows of any alignment copied to rows of a multiple of 8 elements, zeros behind K.
+template <typename T>
+__global__ __launch_bounds__(256) void align_rows_kernel(const T *__restrict__ x, long long ldx, long long chunks, int per_row, int K, T *__restrict__ out) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= chunks) return;
+  const long long row = i / per_row;
+  const int k = (int)(i - row * per_row) * 8;
+  *reinterpret_cast<typename Half<T>::v8 *>(out + i * 8) = row8(x + row * ldx, k, K);
 }
 
 std::atomic<int> g_linear_variant{-1};
 
-struct LinearPlan {
-  int kind, splits, slices;
-};
-//   0 = any 64 x 64   1 = any 128 x 128   2 = rows (M <= 64)
-//   3 = dma 256 x 320, 8 waves   4 = dma 256 x 256, 8 waves   5 = dma 128 x 128   6 = dma 64 x 64
-//   7 = dma 32 x 32, four K groups   8 = dma 64 x 64, two K groups  9 = dma 128 x 128, two K groups
-LinearPlan plan_linear(int M, int N, int K, bool wide, const void *ws, size_t ws_bytes) {
-  int kind;
-  if (M <= 64) kind = 2;
-  else if (!wide) kind = (long long)M * N > 1024 * 1024 ? 1 : 0;
-  else kind = 5;
+// Which kernel:
+//   0, 1 = any alignment, 64 x 64 and 128 x 128 tiles     2 = rows straight to the matrix unit (M <= 16)     10 = vector unit (M <= 4)
+//   direct-to-LDS tiles: 3 = 256 x 320, 4 = 256 x 256 (8 waves, ring of 2)   5 = 128 x 128 (ring of 2, two workgroups a CU)
+//   6 = 64 x 64 (ring of 3)   7 = 32 x 32, 4 K groups   8 = 64 x 64, 2 K groups   9 = 128 x 128, 2 K groups   11 = 32 x 32, 8 K groups
+constexpr int kLinearKinds = 12;
+
+int plan_linear(int M, int N, int K, bool wide) {
   const int forced = g_linear_variant.load(std::memory_order_relaxed);
-  if (forced >= 0 && forced <= 9 && (forced != 2 || M <= 64) && (forced <= 2 || wide)) kind = forced;
-  const int slice = kind <= 1 ? 32 : (kind == 7 || kind == 8 ? 128 : 64), n = (K + slice - 1) / slice;
-  return LinearPlan{kind, 1, n};
+  if (forced >= 0 && forced < kLinearKinds && (forced != 2 || M <= 16) && (forced != 10 || M <= 4) && (forced < 3 || forced == 10 || wide))
+    return forced;
+  if (M <= 2 || (M <= 4 && !wide)) return 10;
+  auto tiles = [&](long long bm, long long bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  const long long t32 = tiles(32, 32), t64 = tiles(64, 64), t128 = tiles(128, 128);
+  if (!wide) return M <= 16 ? 2 : (t128 >= 256 ? 1 : 0);
+  if (t32 <= 256 && K >= 2048) return 11;
+  if (t32 <= 512) return 7;
+  if (t64 <= 256) return 8;
+  if (t64 <= 560) return 6;
+  if (t128 <= 256) return 9;
+  if (t128 <= 512) return 5;
+  // rounds of 256 CUs times the area of a tile; the 128 x 128 ones run two to a CU at 0.9 of the others' rate
+  auto rounds = [](long long t, long long n) { return (double)((t + n - 1) / n); };
+  const double e3 = rounds(tiles(256, 320), 256) * (256.0 * 320.0), e4 = rounds(tiles(256, 256), 256) * (256.0 * 256.0);
+  const double e5 = rounds(t128, 512) * (2.0 * 128.0 * 128.0) * 1.1;
+  return e3 < e4 && e3 < e5 ? 3 : (e4 <= e5 ? 4 : 5);
 }
 
 template <typename T, typename O, int BM, int BN, int WGM, int WGN, int S, int BKB, int OCC, int KG>
-int run_dma(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, const LinearPlan &p, const KRange &kr,
-            hipStream_t st) {
+int run_dma(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, hipStream_t st) {
   constexpr int lds = S * (BM + BN) * BKB;
   // the attribute is per device: one bit per device index, set after the first successful call there
   static std::atomic<unsigned long long> attr_set{0};
@@ -512,30 +572,49 @@ int run_dma(const T *x, long long ldx, const T *W, long long ldw, int M, int N, 
     attr_set.fetch_or(bit, std::memory_order_release);
   }
   const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
-  hipLaunchKernelGGL((linear_dma_kernel<T, O, BM, BN, WGM, WGN, S, BKB, OCC, KG>), dim3(tiles_m * tiles_n, p.splits), dim3(64 * WGM * WGN * KG), lds, st,
-                     x, ldx, W, ldw, M, N, K, epi, tiles_m, tiles_n, kr);
+  hipLaunchKernelGGL((linear_dma_kernel<T, O, BM, BN, WGM, WGN, S, BKB, OCC, KG>), dim3(tiles_m * tiles_n), dim3(64 * WGM * WGN * KG), lds, st,
+                     x, ldx, W, ldw, M, N, K, epi, tiles_m, tiles_n);
   QUAMBA_LAUNCH_CHECK();
   return QUAMBA_OK;
 }
 
 template <typename T, typename O, int TM, int TN>
-int run_any(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, const LinearPlan &p, const KRange &kr,
-            hipStream_t st) {
+int run_any(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, hipStream_t st) {
   const int tiles_m = (M + 64 * TM - 1) / (64 * TM), tiles_n = (N + 64 * TN - 1) / (64 * TN);
-  hipLaunchKernelGGL((linear_any_kernel<T, O, TM, TN>), dim3(tiles_m * tiles_n, p.splits), dim3(256), 0, st, x, ldx, W, ldw, M, N, K, epi, tiles_m,
-                     tiles_n, kr);
+  hipLaunchKernelGGL((linear_any_kernel<T, O, TM, TN>), dim3(tiles_m * tiles_n), dim3(256), 0, st, x, ldx, W, ldw, M, N, K, epi, tiles_m,
+                     tiles_n);
   QUAMBA_LAUNCH_CHECK();
   return QUAMBA_OK;
 }
 
-template <typename T, typename O, int MT>
-int run_rows(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, hipStream_t st) {
-  const dim3 grid((N + 15) / 16);
+template <typename T, typename O, int MR>
+int run_vec(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, hipStream_t st) {
   if (K <= 1024)
-    hipLaunchKernelGGL((linear_rows_kernel<T, O, MT, 4>), grid, dim3(256), 0, st, x, ldx, W, ldw, M, N, K, epi);
+    hipLaunchKernelGGL((linear_vec_kernel<T, O, MR, 64>), dim3((N + 15) / 16), dim3(256), 0, st, x, ldx, W, ldw, M, N, K, epi);
   else
-    hipLaunchKernelGGL((linear_rows_kernel<T, O, MT, 8>), grid, dim3(512), 0, st, x, ldx, W, ldw, M, N, K, epi);
+    hipLaunchKernelGGL((linear_vec_kernel<T, O, MR, 256>), dim3((N + 3) / 4), dim3(256), 0, st, x, ldx, W, ldw, M, N, K, epi);
   QUAMBA_LAUNCH_CHECK();
+  return QUAMBA_OK;
+}
+
+template <typename T>
+bool rows_wide(const T *p, long long ld, int K) {
+  return aligned(p, 16) && ld % 8 == 0 && K % 8 == 0 && ld < (1 << 21);  // a tile's rows lie within 2^31 bytes
+}
+size_t aligned_bytes(int rows, int K) { return align_up((size_t)rows * align_up(K, 8) * 2, 256); }
+// More rows than the streaming kernels take: operands of any alignment are worth copying to 16-byte rows first
+bool copies(int M) { return M > 16; }
+
+template <typename T>
+int align_rows(const T **p, long long *ld, int rows, int K, char **ws, hipStream_t st) {
+  const int per_row = (K + 7) / 8;
+  const long long chunks = (long long)rows * per_row;
+  T *out = reinterpret_cast<T *>(*ws);
+  hipLaunchKernelGGL(align_rows_kernel<T>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, *p, *ld, chunks, per_row, K, out);
+  QUAMBA_LAUNCH_CHECK();
+  *p = out;
+  *ld = per_row * 8LL;
+  *ws += aligned_bytes(rows, K);
   return QUAMBA_OK;
 }
 
@@ -544,31 +623,36 @@ int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int 
                hipStream_t st) {
   if (((M + 31LL) / 32) * ((N + 31LL) / 32) > INT_MAX)
     return fail(QUAMBA_EUNSUPPORTED, "linear: %d x %d outputs are more than one launch takes", M, N);
-  const bool wide = aligned(x, 16) && aligned(W, 16) && ldx % 8 == 0 && ldw % 8 == 0 && K % 8 == 0;
-  const LinearPlan p = plan_linear(M, N, K, wide, ws, ws_bytes);
-  const KRange kr{p.slices, p.splits > 1 ? static_cast<float *>(ws) : nullptr};
-  int rc;
-  switch (p.kind) {
-    case 0: rc = run_any<T, O, 1, 1>(x, ldx, W, ldw, M, N, K, epi, p, kr, st); break;
-    case 1: rc = run_any<T, O, 2, 2>(x, ldx, W, ldw, M, N, K, epi, p, kr, st); break;
-    case 2:
-      if (M <= 16) rc = run_rows<T, O, 1>(x, ldx, W, ldw, M, N, K, epi, st);
-      else if (M <= 32) rc = run_rows<T, O, 2>(x, ldx, W, ldw, M, N, K, epi, st);
-      else rc = run_rows<T, O, 4>(x, ldx, W, ldw, M, N, K, epi, st);
-      break;
-    case 3: rc = run_dma<T, O, 256, 320, 4, 2, 2, 128, 2, 1>(x, ldx, W, ldw, M, N, K, epi, p, kr, st); break;
-    case 4: rc = run_dma<T, O, 256, 256, 4, 2, 2, 128, 2, 1>(x, ldx, W, ldw, M, N, K, epi, p, kr, st); break;
-    case 6: rc = run_dma<T, O, 64, 64, 2, 2, 3, 128, 2, 1>(x, ldx, W, ldw, M, N, K, epi, p, kr, st); break;
-    case 7: rc = run_dma<T, O, 32, 32, 1, 1, 3, 256, 2, 4>(x, ldx, W, ldw, M, N, K, epi, p, kr, st); break;
-    case 8: rc = run_dma<T, O, 64, 64, 2, 2, 3, 256, 2, 2>(x, ldx, W, ldw, M, N, K, epi, p, kr, st); break;
-    case 9: rc = run_dma<T, O, 128, 128, 2, 2, 4, 128, 2, 2>(x, ldx, W, ldw, M, N, K, epi, p, kr, st); break;
-    default: rc = run_dma<T, O, 128, 128, 2, 2, 2, 128, 2, 1>(x, ldx, W, ldw, M, N, K, epi, p, kr, st); break;
+  bool wx = rows_wide(x, ldx, K), ww = rows_wide(W, ldw, K);
+  if (copies(M) && !(wx && ww) && ws && (wx ? 0 : aligned_bytes(M, K)) + (ww ? 0 : aligned_bytes(N, K)) <= ws_bytes &&
+      g_linear_variant.load(std::memory_order_relaxed) < 0) {
+    char *at = static_cast<char *>(ws);
+    int rc = wx ? QUAMBA_OK : align_rows(&x, &ldx, M, K, &at, st);
+    if (rc == QUAMBA_OK && !ww) rc = align_rows(&W, &ldw, N, K, &at, st);
+    if (rc != QUAMBA_OK) return rc;
+    wx = ww = true;
+    K = (int)align_up(K, 8);
   }
-  if (rc != QUAMBA_OK || p.splits == 1) return rc;
-  const size_t n = (size_t)M * N;
-  hipLaunchKernelGGL(linear_join_kernel<O>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, kr.partial, p.splits, M, N, epi);
-  QUAMBA_LAUNCH_CHECK();
-  return QUAMBA_OK;
+  switch (plan_linear(M, N, K, wx && ww)) {
+    case 0: return run_any<T, O, 1, 1>(x, ldx, W, ldw, M, N, K, epi, st);
+    case 1: return run_any<T, O, 2, 2>(x, ldx, W, ldw, M, N, K, epi, st);
+    case 2:
+      hipLaunchKernelGGL((linear_rows_kernel<T, O>), dim3((N + 15) / 16), dim3(512), 0, st, x, ldx, W, ldw, M, N, K, epi);
+      QUAMBA_LAUNCH_CHECK();
+      return QUAMBA_OK;
+    case 3: return run_dma<T, O, 256, 320, 4, 2, 2, 128, 2, 1>(x, ldx, W, ldw, M, N, K, epi, st);
+    case 4: return run_dma<T, O, 256, 256, 4, 2, 2, 128, 2, 1>(x, ldx, W, ldw, M, N, K, epi, st);
+    case 6: return run_dma<T, O, 64, 64, 2, 2, 3, 128, 2, 1>(x, ldx, W, ldw, M, N, K, epi, st);
+    case 7: return run_dma<T, O, 32, 32, 1, 1, 3, 256, 2, 4>(x, ldx, W, ldw, M, N, K, epi, st);
+    case 8: return run_dma<T, O, 64, 64, 2, 2, 3, 256, 2, 2>(x, ldx, W, ldw, M, N, K, epi, st);
+    case 9: return run_dma<T, O, 128, 128, 2, 2, 4, 128, 2, 2>(x, ldx, W, ldw, M, N, K, epi, st);
+    case 10:
+      if (M <= 1) return run_vec<T, O, 1>(x, ldx, W, ldw, M, N, K, epi, st);
+      if (M <= 2) return run_vec<T, O, 2>(x, ldx, W, ldw, M, N, K, epi, st);
+      return run_vec<T, O, 4>(x, ldx, W, ldw, M, N, K, epi, st);
+    case 11: return run_dma<T, O, 32, 32, 1, 1, 3, 512, 2, 8>(x, ldx, W, ldw, M, N, K, epi, st);
+    default: return run_dma<T, O, 128, 128, 2, 2, 2, 128, 2, 1>(x, ldx, W, ldw, M, N, K, epi, st);
+  }
 }
 
 }  // namespace
@@ -584,7 +668,7 @@ size_t quamba_linear_workspace_bytes(int M, int N, int K) {
     fail(QUAMBA_EINVAL, "linear: M=%d N=%d K=%d", M, N, K);
     return 0;
   }
-  return 256;
+  return copies(M) ? aligned_bytes(M, K) + aligned_bytes(N, K) : 256;
 }
 
 int quamba_linear(int type, const void *x, int ldx, const void *W, int ldw, const float *bias, const void *residual, int ldr,
@@ -602,9 +686,8 @@ int quamba_linear(int type, const void *x, int ldx, const void *W, int ldw, cons
   if (!aligned(x, 2) || !aligned(W, 2) || !aligned(out, osz) || !aligned(residual, osz) || !aligned(bias, 4))
     return fail(QUAMBA_EINVAL, "linear: a buffer is not aligned to its elements");
   if (residual == out && ldr != ldo) return fail(QUAMBA_EINVAL, "linear: residual in place with ldr=%d, ldo=%d", ldr, ldo);
-  if (ws && !aligned(ws, 16)) return fail(QUAMBA_EINVAL, "linear: workspace must be 16-byte aligned");
-  const bool wide_rows = aligned(out, 16) && ldo * osz % 16 == 0 && (!residual || (aligned(residual, 16) && ldr * osz % 16 == 0));
-  const LinearEpi e{bias, residual, out, ldr, ldo, act, wide_rows};
+  if (ws && !aligned(ws, 256)) return fail(QUAMBA_EINVAL, "linear: workspace must be 256-byte aligned");
+  const LinearEpi e{bias, residual, out, ldr, ldo, act};
   hipStream_t st = as_stream(stream);
   if (type == QUAMBA_TYPE_F16) {
     const auto *a = static_cast<const _Float16 *>(x), *b = static_cast<const _Float16 *>(W);
