@@ -24,25 +24,40 @@ struct LinearEpi {
   int act;
 };
 
-// The activation is evaluated in fp32.  exp2 of a large positive argument is infinite and its reciprocal 0, so the
-// sigmoid needs no branch; SiLU's v * 0 at v = -inf would be NaN where the limit is -0, as v / (1 + inf) gives.
+// 0.5 erfc(z / sqrt 2) for z >= 0: with y = z / sqrt 2 and t = 1 / (1 + 0.4 y), erfc(y) = exp(-y^2) t p(t), p of degree 8
+// fitted to erfc(y) exp(y^2) / t over 0 < t <= 1 by least squares whose weights were moved towards equal errors (1.3e-7 of the
+// value).  A relative error, so the far tail of GELU is as good as its middle; a third of the instructions of erfcf.
+__device__ __forceinline__ float upper_tail(float z) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.4f * 0.70710678118654752440f, z, 1.f));
+  float p = 0.02512870542705059f;
+  p = fmaf(p, t, -0.09144222736358643f);
+  p = fmaf(p, t, 0.08453038334846497f);
+  p = fmaf(p, t, -0.0027945844922214746f);
+  p = fmaf(p, t, 0.07071199268102646f);
+  p = fmaf(p, t, 0.08427179604768753f);
+  p = fmaf(p, t, 0.10392126441001892f);
+  p = fmaf(p, t, 0.11283480376005173f);
+  p = fmaf(p, t, 0.11283793300390244f);
+  return p * t * __builtin_amdgcn_exp2f(-0.72134752044448170368f * z * z);
+}
+
+// The activation in fp32.  exp2 of a large argument is infinite and its reciprocal 0, so nothing overflows on the way; v * 0 at
+// v = -infinity would be NaN where the limit is 0.
 __device__ __forceinline__ float activate(float v, int act) {
   constexpr float LOG2E = 1.44269504088896340736f;
   switch (act) {
     case QUAMBA_ACT_RELU: return v < 0.f ? 0.f : v;  // keeps NaN
-    case QUAMBA_ACT_SILU: return v == -INFINITY ? 0.f : v / (1.f + __builtin_amdgcn_exp2f(-v * LOG2E));
-    case QUAMBA_ACT_GELU: {
-      // 0.5 v erfc(-v / sqrt 2): no cancellation for negative v, 0 at -inf instead of -inf * 0
-      const float e = erfcf(v * -0.70710678118654752440f);
-      return e == 0.f ? 0.f : 0.5f * v * e;
+    case QUAMBA_ACT_SILU: return v == -INFINITY ? 0.f : v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-v * LOG2E));
+    case QUAMBA_ACT_GELU: {  // v Phi(v)
+      const float u = upper_tail(fabsf(v)), phi = v < 0.f ? u : 1.f - u;
+      return phi == 0.f ? 0.f : v * phi;
     }
-    case QUAMBA_ACT_GELU_TANH: {
-      // 0.5 v (1 + tanh u) = v sigmoid(2 u), u = sqrt(2 / pi) (v + 0.044715 v^3)
+    case QUAMBA_ACT_GELU_TANH: {  // 0.5 v (1 + tanh u) = v sigmoid(2 u), u = sqrt(2 / pi) (v + 0.044715 v^3)
       const float u2 = 1.59576912160573071176f * v * (1.f + 0.044715f * v * v);
-      const float d = 1.f + __builtin_amdgcn_exp2f(-u2 * LOG2E);
-      return d == INFINITY ? 0.f : v / d;
+      const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-u2 * LOG2E));
+      return s == 0.f ? 0.f : v * s;
     }
-    case QUAMBA_ACT_SIGMOID: return 1.f / (1.f + __builtin_amdgcn_exp2f(-v * LOG2E));
+    case QUAMBA_ACT_SIGMOID: return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-v * LOG2E));
     default: return v;
   }
 }
@@ -75,11 +90,11 @@ __device__ __forceinline__ int swz(int row, int chunk) {
 }
 
 // A wave's TM x TN tiles of 32 x 32 sums: register r of lane l in tile (i, j) is column n_base + 32 i + 8 (r / 4) + 4 (l / 32)
-// + r % 4 of row m_base + 32 j + l % 32.  A band of 32 rows and up to 64 columns at a time goes through a region of LDS that
-// only this wave uses (fp32, rows 16 bytes further apart than they are long), so that bias, residual and output are
-// taken 16 bytes a lane along the rows (global memory takes such accesses at any element's address).  A band's residual is asked
-// for before its sums are laid out; one trip per row after them cost 4 us of a 22 us call.  The activation is a pass of its own
-// over the band: its code exists once.
+// + r % 4 of row m_base + 32 j + l % 32.  A tile gets its bias and activation in registers (after a copy, so that their code
+// exists once), then a band of 32 rows and up to 64 columns goes through a region of LDS that only this wave uses (fp32, rows 16
+// bytes further apart than they are long), so that residual and output are taken 16 bytes a lane along the rows (global memory
+// takes such accesses at any element's address).  The residual is asked for before the sums are laid out: one trip per row after
+// them cost 4 us of a 22 us call.
 constexpr int kBandPitch = 64 * 4 + 16;
 constexpr int kBandBytes = 32 * kBandPitch;
 
@@ -87,17 +102,13 @@ template <typename O>
 struct Band {
   static constexpr int E = 16 / sizeof(O), IT = 32 * 64 / (64 * E);  // elements of a 16-byte access; accesses of a lane (64 columns)
   typedef O vO __attribute__((ext_vector_type(E)));
-  int m0, n0, per_row, cc, gn, r0, rows;  // the lane's columns cc ..; rows r0, r0 + rows, ...
-  bool whole;
-  float bias[E];
+  int m0, cc, gn, r0, rows;  // the lane's columns cc .., gn .. of the output; rows r0, r0 + rows, ...
   vO res[IT];
 
   __device__ __forceinline__ void ask(const LinearEpi &e, int m, int n, int cols, int lane, int M, int N) {
-    m0 = m, n0 = n, per_row = cols / E, cc = lane % per_row * E, gn = n0 + cc, r0 = lane / per_row, rows = 64 / per_row;
-    whole = gn + E <= N;
-#pragma unroll
-    for (int i = 0; i < E; ++i) bias[i] = e.bias && gn + i < N ? e.bias[gn + i] : 0.f;
-    if (e.res && whole) {
+    const int per_row = cols / E;
+    m0 = m, cc = lane % per_row * E, gn = n + cc, r0 = lane / per_row, rows = 64 / per_row;
+    if (e.res && gn + E <= N) {
 #pragma unroll
       for (int it = 0; it < IT; ++it) {
         const int r = r0 + it * rows;
@@ -105,19 +116,7 @@ struct Band {
       }
     }
   }
-  __device__ __forceinline__ void put(const LinearEpi &e, int M, int N, char *band) const {
-    if (e.act != QUAMBA_ACT_NONE) {
-#pragma unroll 1
-      for (int r = r0; r < 32; r += rows)
-#pragma unroll
-        for (int i = 0; i < E; i += 4) {
-          v4f *p = reinterpret_cast<v4f *>(band + r * kBandPitch + (cc + i) * 4);
-          v4f t = *p;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) t[c] = activate(t[c] + bias[i + c], e.act);
-          *p = t;
-        }
-    }
+  __device__ __forceinline__ void put(const LinearEpi &e, int M, int N, const char *band) const {
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
       const int r = r0 + it * rows, gm = m0 + r;
@@ -127,10 +126,10 @@ struct Band {
       for (int i = 0; i < E; i += 4) {
         const v4f t = *reinterpret_cast<const v4f *>(band + r * kBandPitch + (cc + i) * 4);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) v[i + c] = e.act != QUAMBA_ACT_NONE ? t[c] : t[c] + bias[i + c];
+        for (int c = 0; c < 4; ++c) v[i + c] = t[c];
       }
       O *out = static_cast<O *>(e.out) + (size_t)gm * e.ldo + gn;
-      if (whole) {
+      if (gn + E <= N) {
         vO t;
 #pragma unroll
         for (int i = 0; i < E; ++i) t[i] = from_f32<O>(e.res ? v[i] + to_f32(res[it][i]) : v[i]);
@@ -148,23 +147,47 @@ struct Band {
 template <typename O, int TM, int TN>
 __device__ __forceinline__ void store_wave(const v16f (&acc)[TN][TM], int m_base, int n_base, int lane, int M, int N, const LinearEpi &e,
                                            char *band) {
-  constexpr int PER = (TN + 1) / 2;  // bands of columns
+  Band<O> b;
 #pragma unroll 1
-  for (int step = 0; step < TM * PER; ++step) {
-    const int j = step / PER, i0 = step % PER * 2;
-    Band<O> b;
-    b.ask(e, m_base + 32 * j, n_base + 32 * i0, i0 + 1 < TN ? 64 : 32, lane, M, N);
+  for (int step = 0; step < TM * TN; ++step) {
+    const int j = step / TN, i = step - j * TN;
+    const bool first = (i & 1) == 0, last = !first || i + 1 == TN;
+    if (first) b.ask(e, m_base + 32 * j, n_base + 32 * i, i + 1 < TN ? 64 : 32, lane, M, N);
+    float v[16], bias[16];
+    if (e.bias) {
 #pragma unroll
-    for (int s = 0; s < TM * PER; ++s)
+      for (int r = 0; r < 16; ++r) bias[r] = e.bias[min(n_base + 32 * i + 4 * (lane >> 5) + 8 * (r / 4) + r % 4, N - 1)];
+    }
+#pragma unroll
+    for (int s = 0; s < TM * TN; ++s)
       if (s == step) {
+        asm volatile("");  // a branch: as selects these are TM TN 16 instructions a step (19 us of a 118 us call)
 #pragma unroll
-        for (int i = s % PER * 2; i < TN && i < s % PER * 2 + 2; ++i)
-#pragma unroll
-          for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<v4f *>(band + (lane & 31) * kBandPitch + ((i & 1) * 32 + 8 * g + 4 * (lane >> 5)) * 4) =
-                v4f{acc[i][s / PER][4 * g], acc[i][s / PER][4 * g + 1], acc[i][s / PER][4 * g + 2], acc[i][s / PER][4 * g + 3]};
+        for (int r = 0; r < 16; ++r) v[r] = acc[s % TN][s / TN][r];
       }
-    b.put(e, M, N, band);
+    if (e.bias) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) v[r] += bias[r];
+    }
+    switch (e.act) {
+#define QUAMBA_ALL(A)                                  \
+  case A: {                                            \
+    _Pragma("unroll") for (int r = 0; r < 16; ++r) v[r] = activate(v[r], A); \
+    break;                                             \
+  }
+      QUAMBA_ALL(QUAMBA_ACT_RELU)
+      QUAMBA_ALL(QUAMBA_ACT_SILU)
+      QUAMBA_ALL(QUAMBA_ACT_GELU)
+      QUAMBA_ALL(QUAMBA_ACT_GELU_TANH)
+      QUAMBA_ALL(QUAMBA_ACT_SIGMOID)
+#undef QUAMBA_ALL
+      default: break;
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<v4f *>(band + (lane & 31) * kBandPitch + ((i & 1) * 32 + 8 * g + 4 * (lane >> 5)) * 4) =
+          v4f{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+    if (last) b.put(e, M, N, band);
   }
 }
 
@@ -519,7 +542,7 @@ __global__ __launch_bounds__(256) void linear_vec_kernel(const T *__restrict__ x
     put1<O>(epi, one, gm, gn, LANES == 64 ? part[wave][mine] : part[0][mine] + part[1][mine] + part[2][mine] + part[3][mine]);
 }
 
-// Rows of any alignment copied to rows of a multiple of 8 elements, zeros behind K.
+// Rows of any alignment copied to rows of a multiple of 64 elements, zeros behind K.
 template <typename T>
 __global__ __launch_bounds__(256) void align_rows_kernel(const T *__restrict__ x, long long ldx, long long chunks, int per_row, int K, T *__restrict__ out) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -601,13 +624,14 @@ template <typename T>
 bool rows_wide(const T *p, long long ld, int K) {
   return aligned(p, 16) && ld % 8 == 0 && K % 8 == 0 && ld < (1 << 21);  // a tile's rows lie within 2^31 bytes
 }
-size_t aligned_bytes(int rows, int K) { return align_up((size_t)rows * align_up(K, 8) * 2, 256); }
+constexpr int kCopyUnit = 64;  // elements a copied row is a multiple of: whole 128-byte lines
+size_t aligned_bytes(int rows, int K) { return align_up((size_t)rows * align_up(K, kCopyUnit) * 2, 256); }
 // More rows than the streaming kernels take: operands of any alignment are worth copying to 16-byte rows first
 bool copies(int M) { return M > 16; }
 
 template <typename T>
 int align_rows(const T **p, long long *ld, int rows, int K, char **ws, hipStream_t st) {
-  const int per_row = (K + 7) / 8;
+  const int per_row = (int)align_up(K, kCopyUnit) / 8;
   const long long chunks = (long long)rows * per_row;
   T *out = reinterpret_cast<T *>(*ws);
   hipLaunchKernelGGL(align_rows_kernel<T>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, *p, *ld, chunks, per_row, K, out);
@@ -631,7 +655,7 @@ int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int 
     if (rc == QUAMBA_OK && !ww) rc = align_rows(&W, &ldw, N, K, &at, st);
     if (rc != QUAMBA_OK) return rc;
     wx = ww = true;
-    K = (int)align_up(K, 8);
+    K = (int)align_up(K, kCopyUnit);
   }
   switch (plan_linear(M, N, K, wx && ww)) {
     case 0: return run_any<T, O, 1, 1>(x, ldx, W, ldw, M, N, K, epi, st);
