@@ -531,27 +531,40 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
           sf[n] = pow2(se[n]);
         }
       }
+      // operands of step j + 1 are asked for, and its pieces of S made, under the products of step j: left to itself the compiler
+      // reads each operand right before its product and waits for it
+      v8 fq[2][4];
+      u4 sh[2][NT], sl[2][NT];
+      auto ask_q = [&](int j, v8 (&f)[4]) {
 #pragma unroll
-      for (int j = 0; j < KT; ++j) {
-        u4 sh[NT], sl[NT];
+        for (int tb = 0; tb < 4; ++tb) f[tb] = row_operand<T, KT>(lq, at_row, tb, j);
+      };
+      auto split = [&](int j, u4 (&hi)[NT], u4 (&lo)[NT]) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 8; e += 2) {
             float x = S[2 * j + (e >> 2)][n][e & 3], y = S[2 * j + (e >> 2)][n][(e & 3) + 1];
             if constexpr (F16) x *= sf[n], y *= sf[n];
-            sh[n][e / 2] = take2(x, y, T());
-            sl[n][e / 2] = pack2<T>(x, y);
+            hi[n][e / 2] = take2(x, y, T());
+            lo[n][e / 2] = pack2<T>(x, y);
           }
+      };
+      ask_q(0, fq[0]);
+      split(0, sh[0], sl[0]);
 #pragma unroll
-        for (int tb = 0; tb < 4; ++tb) {
-          const v8 fq = row_operand<T, KT>(lq, at_row, tb, j);
+      for (int j = 0; j < KT; ++j) {
+        if (j + 1 < KT) ask_q(j + 1, fq[(j + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            O[tb][n] = Half<T>::mfma16(__builtin_bit_cast(v8, sh[n]), fq, O[tb][n]);
-            O[tb][n] = Half<T>::mfma16(__builtin_bit_cast(v8, sl[n]), fq, O[tb][n]);
-          }
-        }
+        for (int tb = 0; tb < 4; ++tb)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) O[tb][n] = Half<T>::mfma16(__builtin_bit_cast(v8, sh[j & 1][n]), fq[j & 1][tb], O[tb][n]);
+        if (j + 1 < KT) split(j + 1, sh[(j + 1) & 1], sl[(j + 1) & 1]);
+#pragma unroll
+        for (int tb = 0; tb < 4; ++tb)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) O[tb][n] = Half<T>::mfma16(__builtin_bit_cast(v8, sl[j & 1][n]), fq[j & 1][tb], O[tb][n]);
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -608,18 +621,27 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
             vh[kb][n] = fv[kb][n];
           }
         }
-#pragma unroll
-      for (int tb = 0; tb < 4; ++tb) {
+      b8 ph[2][2], pl[2][2];
+      auto ask_p = [&](int tb) {
 #pragma unroll
         for (int kb = 0; kb <= tb / 2; ++kb) {
-          const b8 ph = weight_operand(lp, 16 * tb + c, kb, lane), pl = weight_operand(lpl, 16 * tb + c, kb, lane);
+          ph[tb & 1][kb] = weight_operand(lp, 16 * tb + c, kb, lane);
+          pl[tb & 1][kb] = weight_operand(lpl, 16 * tb + c, kb, lane);
+        }
+      };
+      ask_p(0);
+#pragma unroll
+      for (int tb = 0; tb < 4; ++tb) {
+        if (tb < 3) ask_p(tb + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kb = 0; kb <= tb / 2; ++kb)
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            O[tb][n] = Half<__bf16>::mfma16(vh[kb][n], ph, O[tb][n]);
-            O[tb][n] = Half<__bf16>::mfma16(vh[kb][n], pl, O[tb][n]);
-            if constexpr (F16) O[tb][n] = Half<__bf16>::mfma16(vl[kb][n], ph, O[tb][n]);
+            O[tb][n] = Half<__bf16>::mfma16(vh[kb][n], ph[tb & 1][kb], O[tb][n]);
+            O[tb][n] = Half<__bf16>::mfma16(vh[kb][n], pl[tb & 1][kb], O[tb][n]);
+            if constexpr (F16) O[tb][n] = Half<__bf16>::mfma16(vl[kb][n], ph[tb & 1][kb], O[tb][n]);
           }
-        }
         const int t = t0 + 16 * tb + c;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -675,9 +697,16 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
         }
     }
     const float dec = tab.dec;
+    v8 fk[2][2];
+    auto ask_k = [&](int i) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) fk[i & 1][kb] = column_operand<T, KT>(lks, at_column, kb, i);
+    };
+    ask_k(0);
 #pragma unroll
     for (int i = 0; i < 2 * KT; ++i) {
-      const v8 k0 = column_operand<T, KT>(lks, at_column, 0, i), k1 = column_operand<T, KT>(lks, at_column, 1, i);
+      if (i + 1 < 2 * KT) ask_k(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
       v4f u[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -686,10 +715,9 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 #pragma unroll
       for (int p = VP - 1; p >= 0; --p)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          u[n] = Half<T>::mfma16(k0, __builtin_bit_cast(v8, wv[p][0][n]), u[n]);
-          u[n] = Half<T>::mfma16(k1, __builtin_bit_cast(v8, wv[p][1][n]), u[n]);
-        }
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) u[n] = Half<T>::mfma16(fk[i & 1][kb], __builtin_bit_cast(v8, wv[p][kb][n]), u[n]);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
