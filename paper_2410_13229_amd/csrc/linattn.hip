@@ -309,6 +309,18 @@ __device__ __forceinline__ unsigned take2(float &a, float &b, _Float16) {
 }
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
+// 16 bytes a lane from base + off (lane) + soff (wave) to consecutive LDS from `to` on, zeros where off is negative.  Written
+// out, because the compiler takes every LDS read for one of what such a load is still bringing and waits for the load first (three
+// times a block; 2 x 4000, 32 heads of 64 x 64: 72 -> 67 us).  What it would know is kept by hand: nothing reads a tile before
+// block_barrier<true>, and the scalar operands may come straight from a vector instruction, hence the five wait states (and m0
+// is nobody else's: of what the compiler writes here, only its own direct-to-LDS loads would use it).
+__device__ __forceinline__ void tile_load(const void *base, int off, int soff, const char *to) {
+  const unsigned long long b = reinterpret_cast<unsigned long long>(base);
+  const u4 rsrc = {(unsigned)b, (unsigned)(b >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
+  const unsigned lds = (unsigned)reinterpret_cast<unsigned long long>((const __attribute__((address_space(3))) char *)to);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(off), "s"(rsrc), "s"(soff));
+}
+
 // Order LDS accesses (the compiler's and the wave's own) around the hardware barrier.  VM: the wave's direct-to-LDS loads have
 // landed too.
 template <bool VM>
@@ -386,7 +398,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
       const int n = t_hi - t0;  // rows that count
       if constexpr (WIDE) {
         const int off = n >= kBlock || tile_row(i) < n ? o[i % PH] : OFF;
-        load_to_lds(buffer_over(p + (size_t)t0 * ld, 0x7fffffff), off, (int)((i / PH) * (PH * 4 * RPL) * ld * 2), tile + ((i / PH) * PH * 4 + (i % PH) * 4 + wave) * 1024);
+        tile_load(p + (size_t)t0 * ld, off, (int)((i / PH) * (PH * 4 * RPL) * ld * 2), tile + ((i / PH) * PH * 4 + (i % PH) * 4 + wave) * 1024);
       } else {
         r[i] = tile_row(i) < n ? row8(p + (size_t)(t0 + tile_row(i)) * ld, tile_chunk(i) * 8, a.dk) : zero;
       }
@@ -397,7 +409,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
     for (int i = 0; i < NLV; ++i) {
       const int n = t_hi - t0, row = v_row + RPLV * i;
       if constexpr (WIDE)
-        load_to_lds(buffer_over(pv + (size_t)t0 * a.ldv, 0x7fffffff), n >= kBlock || row < n ? ov : OFF, (int)(RPLV * i * a.ldv * 2), lv + i * 1024);
+        tile_load(pv + (size_t)t0 * a.ldv, n >= kBlock || row < n ? ov : OFF, (int)(RPLV * i * a.ldv * 2), lv + i * 1024);
       else
         rv[i] = row < n ? row8(pv + (size_t)(t0 + row) * a.ldv, col0 + v_chunk * 8, a.dv) : zero;
     }
