@@ -312,7 +312,7 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 // 16 bytes a lane from base + off (lane) + soff (wave) to consecutive LDS from `to` on, zeros where off is negative.  Written
 // out, because the compiler takes every LDS read for one of what such a load is still bringing and waits for the load first (three
 // times a block; 2 x 4000, 32 heads of 64 x 64: 72 -> 67 us).  What it would know is kept by hand: nothing reads a tile before
-// block_barrier<true>, and the scalar operands may come straight from a vector instruction, hence the five wait states (and m0
+// the barrier that waits for its loads, and the scalar operands may come straight from a vector instruction, hence the five wait states (and m0
 // is nobody else's: of what the compiler writes here, only its own direct-to-LDS loads would use it).
 __device__ __forceinline__ void tile_load(const void *base, int off, int soff, const char *to) {
   const unsigned long long b = reinterpret_cast<unsigned long long>(base);
@@ -321,12 +321,12 @@ __device__ __forceinline__ void tile_load(const void *base, int off, int soff, c
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(off), "s"(rsrc), "s"(soff));
 }
 
-// Order LDS accesses (the compiler's and the wave's own) around the hardware barrier.  VM: the wave's direct-to-LDS loads have
-// landed too.
-template <bool VM>
+// Order LDS accesses (the compiler's and the wave's own) around the hardware barrier.  VM: so many of the wave's vector memory
+// operations, the youngest, may still be under way (they complete in the order of issue); 63: all.
+template <int VM>
 __device__ __forceinline__ void block_barrier() {
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(VM ? 0x0070 : 0xC07F);  // (vmcnt 0 and) lgkmcnt 0, the rest not waited for
+  __builtin_amdgcn_s_waitcnt((VM & 15) | ((VM >> 4) << 14) | 0x0070);  // vmcnt in bits 3:0 and 15:14, lgkmcnt (11:8) 0
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -392,27 +392,29 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
   }
   v8 rq[!WIDE && OUT ? NL : 1], rk[!WIDE ? NL : 1], rv[!WIDE ? NLV : 1];
   const v8 zero = {};
+  auto load_tile = [&](const T *p, long long ld, const int (&o)[PH], v8 *r, int t0, char *tile, int i) {  // load i of the wave's NL
+    const int n = t_hi - t0;  // rows that count
+    if constexpr (WIDE) {
+      const int off = n >= kBlock || tile_row(i) < n ? o[i % PH] : OFF;
+      tile_load(p + (size_t)t0 * ld, off, (int)((i / PH) * (PH * 4 * RPL) * ld * 2), tile + ((i / PH) * PH * 4 + (i % PH) * 4 + wave) * 1024);
+    } else {
+      r[i] = tile_row(i) < n ? row8(p + (size_t)(t0 + tile_row(i)) * ld, tile_chunk(i) * 8, a.dk) : zero;
+    }
+  };
+  auto load_v = [&](int t0, int i) {  // of NLV
+    const int n = t_hi - t0, row = v_row + RPLV * i;
+    if constexpr (WIDE)
+      tile_load(pv + (size_t)t0 * a.ldv, n >= kBlock || row < n ? ov : OFF, (int)(RPLV * i * a.ldv * 2), lv + i * 1024);
+    else
+      rv[i] = row < n ? row8(pv + (size_t)(t0 + row) * a.ldv, col0 + v_chunk * 8, a.dv) : zero;
+  };
   auto fetch_tile = [&](const T *p, long long ld, const int (&o)[PH], v8 *r, int t0, char *tile) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int n = t_hi - t0;  // rows that count
-      if constexpr (WIDE) {
-        const int off = n >= kBlock || tile_row(i) < n ? o[i % PH] : OFF;
-        tile_load(p + (size_t)t0 * ld, off, (int)((i / PH) * (PH * 4 * RPL) * ld * 2), tile + ((i / PH) * PH * 4 + (i % PH) * 4 + wave) * 1024);
-      } else {
-        r[i] = tile_row(i) < n ? row8(p + (size_t)(t0 + tile_row(i)) * ld, tile_chunk(i) * 8, a.dk) : zero;
-      }
-    }
+    for (int i = 0; i < NL; ++i) load_tile(p, ld, o, r, t0, tile, i);
   };
   auto fetch_v = [&](int t0) {
 #pragma unroll
-    for (int i = 0; i < NLV; ++i) {
-      const int n = t_hi - t0, row = v_row + RPLV * i;
-      if constexpr (WIDE)
-        tile_load(pv + (size_t)t0 * a.ldv, n >= kBlock || row < n ? ov : OFF, (int)(RPLV * i * a.ldv * 2), lv + i * 1024);
-      else
-        rv[i] = row < n ? row8(pv + (size_t)(t0 + row) * a.ldv, col0 + v_chunk * 8, a.dv) : zero;
-    }
+    for (int i = 0; i < NLV; ++i) load_v(t0, i);
   };
   auto park = [&](char *lk) {  // what came through registers
     if constexpr (!WIDE) {
@@ -461,7 +463,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
   int resets = 0;
   if (wave == 0) make_table(gt, a.scale, 1.0, lane, tables[0]);
   park(lks);
-  block_barrier<true>();
+  block_barrier<0>();
 
   int buf = 0;
   for (int t0 = t_lo; t0 < t_hi; t0 += kBlock, buf ^= 1) {
@@ -473,56 +475,64 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
     char *lk_next = lks + (buf ^ 1) * TB;
     const int t1 = t0 + kBlock;
     const bool more = t1 < t_hi;
+    // A wave waits about 200 cycles to issue a load while all eight waves of the CU issue theirs: the next block's travel one at a
+    // time between products, k's under the state's contribution, q's under the weights', v's under the update.  The wave that
+    // makes the next table (they take turns) reads the decays.
+    constexpr bool SPREAD = WIDE && OUT;
+    const int maker = OUT ? 2 + ((t0 / kBlock) & 1) : (t0 / kBlock) & 3;
     if (more) {
-      fetch_tile(pk, a.ldk, ok, rk, t1, lk_next);
+      if (wave == maker) gt = log_decay(t1);
+      if constexpr (!SPREAD) fetch_tile(pk, a.ldk, ok, rk, t1, lk_next);
       if constexpr (!WIDE) {
         if constexpr (OUT) fetch_tile(pq, a.ldq, oq, rq, t1, lq);
         fetch_v(t1);
       }
-      gt = log_decay(t1);
     }
 
     v4f O[4][NT];  // transposed: columns (of v) 4 g + r, token 16 tb + c
     if constexpr (OUT) {
-      // weights: the 10 blocks of 16 x 16 on and below the diagonal, three for waves 0 and 1, two for waves 2 and 3, which make the
-      // next block's table in turn
-      auto weights = [&](int id10) {
-        const int tb = id10 < 1 ? 0 : (id10 < 3 ? 1 : (id10 < 6 ? 2 : 3)), sb = id10 - tb * (tb + 1) / 2;
-        v4f p = {0.f, 0.f, 0.f, 0.f};
+      // weights: the 10 blocks of 16 x 16 on and below the diagonal: two with the same tokens t for each wave (sb, sb + 1 of tb: 3 3,
+      // 2 and 1 for the waves), then (0, 0) and (2, 2) for waves 0 and 1, while waves 2 and 3 make the next block's table in turn
+      auto weights = [&](int tb, int sb, auto blocks) {
+        constexpr int B = decltype(blocks)::value;
+        v4f p[B];
+#pragma unroll
+        for (int x = 0; x < B; ++x) p[x] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < KT; ++j) {
           const int at = at_chunk ^ (j << 6);
-          const v8 fk = *reinterpret_cast<const v8 *>(lks + buf * TB + 16 * sb * 64 * KT + at);
           const v8 fq = *reinterpret_cast<const v8 *>(lq + 16 * tb * 64 * KT + at);
-          p = Half<T>::mfma16(fk, fq, p);  // rows s, columns t
-        }
-        const int t = 16 * tb + c, s = 16 * sb + 4 * g;
-        const float dt = tab.d[t] + tab.between[4 * tb + sb];
-        const int nt = tab.n[t];
-        const v4f ds = *reinterpret_cast<const v4f *>(&tab.d[s]);
-        const int4 ns = *reinterpret_cast<const int4 *>(&tab.n[s]);
-        const int nn[4] = {ns.x, ns.y, ns.z, ns.w};
-        const int first = tb != sb ? -1 : 4 * g - c;  // s - t of r = 0, or anything negative enough
-        float v[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const bool on = first + (tb != sb ? 0 : r) <= 0 && nn[r] == nt;
-          v[r] = on ? a.scale * p[r] * __builtin_amdgcn_exp2f(dt - ds[r]) : 0.f;
+          for (int x = 0; x < B; ++x)
+            p[x] = Half<T>::mfma16(*reinterpret_cast<const v8 *>(lks + buf * TB + 16 * (sb + x) * 64 * KT + at), fq, p[x]);  // rows s, columns t
         }
-        const int at = weight_at(t, 2 * sb + (g >> 1)) + (g & 1) * 8;
-        uint2 w;
-        w.x = take2(v[0], v[1], __bf16());
-        w.y = take2(v[2], v[3], __bf16());
-        *reinterpret_cast<uint2 *>(lp + at) = w;
-        w.x = pack2<__bf16>(v[0], v[1]);
-        w.y = pack2<__bf16>(v[2], v[3]);
-        *reinterpret_cast<uint2 *>(lpl + at) = w;
+        const int t = 16 * tb + c;
+        const float d_t = tab.d[t];
+        const int n_t = tab.n[t];
+#pragma unroll
+        for (int x = 0; x < B; ++x) {
+          const int s = 16 * (sb + x) + 4 * g;
+          const float dt = d_t + tab.between[4 * tb + sb + x];
+          const v4f ds = *reinterpret_cast<const v4f *>(&tab.d[s]);
+          const int4 ns = *reinterpret_cast<const int4 *>(&tab.n[s]);
+          const int nn[4] = {ns.x, ns.y, ns.z, ns.w};
+          float v[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = s + r <= t && nn[r] == n_t ? a.scale * p[x][r] * __builtin_amdgcn_exp2f(dt - ds[r]) : 0.f;
+          const int at = weight_at(t, 2 * (sb + x) + (g >> 1)) + (g & 1) * 8;
+          uint2 w;
+          w.x = take2(v[0], v[1], __bf16());
+          w.y = take2(v[2], v[3], __bf16());
+          *reinterpret_cast<uint2 *>(lp + at) = w;
+          w.x = pack2<__bf16>(v[0], v[1]);
+          w.y = pack2<__bf16>(v[2], v[3]);
+          *reinterpret_cast<uint2 *>(lpl + at) = w;
+        }
       };
-      weights(wave);
-      weights(wave + 4);
+      weights(wave < 2 ? 3 : 4 - wave, wave == 1 ? 2 : 0, std::integral_constant<int, 2>());
       if (wave < 2)
-        weights(wave + 8);
-      else if (more && wave - 2 == ((t0 / kBlock) & 1))
+        weights(2 * wave, 2 * wave, std::integral_constant<int, 1>());
+      else if (more && wave == maker)
         make_table(gt, a.scale, tab.carry, lane, tables[buf ^ 1]);
       // what the state contributes
 #pragma unroll
@@ -567,6 +577,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 #pragma unroll
       for (int j = 0; j < KT; ++j) {
         if (j + 1 < KT) ask_q(j + 1, fq[(j + 1) & 1]);
+        if (SPREAD && more) load_tile(pk, a.ldk, ok, rk, t1, lk_next, j);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb)
@@ -594,13 +605,19 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
       }
     }
     if constexpr (!OUT) {
-      if (more && wave == ((t0 / kBlock) & 3)) make_table(gt, a.scale, tab.carry, lane, tables[buf ^ 1]);  // the next block's, by each wave in turn
+      if (more && wave == maker) make_table(gt, a.scale, tab.carry, lane, tables[buf ^ 1]);
       G += tab.sum;
       resets += tab.resets;
     }
     if constexpr (OUT) {
-      block_barrier<false>();  // the weights are in LDS, q is done with
-      if (WIDE && more) fetch_tile(pq, a.ldq, oq, rq, t1, lq);
+      // The weights are in LDS, q is done with, and this wave's v is there: loads complete in order, so where a v load is under way
+      // the KT k loads behind it are too (in the last block there are none).
+      if (!SPREAD)
+        block_barrier<63>();
+      else if (more)
+        block_barrier<KT>();
+      else
+        block_barrier<0>();
     }
 
     v8 fv[2][NT];
@@ -615,7 +632,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int n = 0; n < NT; ++n) asm volatile("" : "+v"(fv[kb][n])::"memory");  // read before the next block's may arrive
-      fetch_v(t1);
+      if constexpr (!SPREAD) fetch_v(t1);
     }
     if constexpr (OUT) {
       b8 vh[2][NT], vl[F16 ? 2 : 1][F16 ? NT : 1];
@@ -645,6 +662,10 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 #pragma unroll
       for (int tb = 0; tb < 4; ++tb) {
         if (tb < 3) ask_p(tb + 1);
+        if (SPREAD && more) {
+#pragma unroll
+          for (int i = tb * KT / 4; i < (tb + 1) * KT / 4; ++i) load_tile(pq, a.ldq, oq, rq, t1, lq, i);
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kb = 0; kb <= tb / 2; ++kb)
@@ -718,6 +739,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 #pragma unroll
     for (int i = 0; i < 2 * KT; ++i) {
       if (i + 1 < 2 * KT) ask_k(i + 1);
+      if (SPREAD && more && i < NLV) load_v(t1, i);
       __builtin_amdgcn_sched_barrier(0);
       v4f u[NT];
 #pragma unroll
@@ -736,7 +758,9 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
         for (int r = 0; r < 4; ++r) S[i][n][r] = F16 ? fmaf(u[n][r], back[n], S[i][n][r] * dec) : u[n][r];
     }
     if (more) park(lk_next);
-    block_barrier<true>();  // the next block's tiles are in LDS, this one's are done with
+    // The next block's k and q are in LDS (where one of their loads is under way the NLV v loads behind it are too), this one's are
+    // done with.
+    block_barrier<SPREAD ? NLV : 0>();
   }
 
   if constexpr (!OUT) {
