@@ -677,6 +677,8 @@ int quamba_probe_rate(int probe, int waves_per_simd, int iters, double *instr_pe
  *                                      launch where served)
  *   quamba_debug_set_linear_variant(v) v >= 0 forces kernel configuration v (0..11) of quamba_linear where the shape
  *                                      allows it; -1 = chosen per shape (default); sums are added in another order
+ *   quamba_debug_set_linattn_blocks(v) v > 0 cuts the prompts of quamba_linattn_prefill into segments of v blocks of 64 tokens
+ *                                      (the workspace query follows); 0 = chosen per shape (default); sums are added in another order
  * Host-only queries of what is chosen for a shape with the full workspace, for tests of the rules:
  *   quamba_debug_gemm_kind(M, N, K)    configuration of an int8 GEMM as quamba_debug_set_gemm_variant counts
  *                                      them, before the launcher cuts rows; -1 = few-row streaming kernel, -2 = not served
@@ -704,6 +706,7 @@ void quamba_debug_set_fuse_decode(int v);
 void quamba_debug_set_scan_variant(int v);
 void quamba_debug_set_decode_stack(int v);
 void quamba_debug_set_linear_variant(int v);
+void quamba_debug_set_linattn_blocks(int v);
 int quamba_debug_gemm_kind(int M, int N, int K);
 int quamba_debug_xfmt_column_tiles(int M, int N, int K);
 int quamba_debug_decode_stack_words(int d_model, int d_inner, int dt_rank, int batch, int role, int item, int32_t *out, int cap);

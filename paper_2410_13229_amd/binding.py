@@ -31,7 +31,8 @@ __all__ = [
     "quamba_linear_workspace_bytes", "quamba_linear", "quamba_linattn_workspace_bytes", "quamba_linattn_prefill", "quamba_linattn_step",
     "quamba_debug_set_gemm_variant", "quamba_debug_set_gemm_split", "quamba_debug_set_gemv_max_rows",
     "quamba_debug_set_fuse_dt", "quamba_debug_set_fuse_decode", "quamba_debug_set_scan_variant",
-    "quamba_debug_set_decode_stack", "quamba_debug_set_linear_variant", "quamba_debug_gemm_kind", "quamba_debug_xfmt_column_tiles", "quamba_debug_last_block_reads_ahead",
+    "quamba_debug_set_decode_stack", "quamba_debug_set_linear_variant", "quamba_debug_set_linattn_blocks",
+    "quamba_debug_gemm_kind", "quamba_debug_xfmt_column_tiles", "quamba_debug_last_block_reads_ahead",
     "quamba_debug_decode_stack_words", "quamba_debug_decode_stack_served",
     "quamba_debug_decode_reads_ahead", "quamba_debug_percentile_workgroups",
     "PROBE_FMA_F32", "PROBE_EXP_F32", "PROBE_SCAN_MIX", "PROBE_MFMA_I8", "PROBE_MFMA_I8_RANDOM",
@@ -365,7 +366,7 @@ def lib():
         getattr(L, name).restype = C.c_int
     for name in ("quamba_debug_set_gemm_variant", "quamba_debug_set_gemm_split", "quamba_debug_set_gemv_max_rows",
                  "quamba_debug_set_fuse_dt", "quamba_debug_set_fuse_decode", "quamba_debug_set_scan_variant",
-                 "quamba_debug_set_decode_stack", "quamba_debug_set_linear_variant"):
+                 "quamba_debug_set_decode_stack", "quamba_debug_set_linear_variant", "quamba_debug_set_linattn_blocks"):
         getattr(L, name).argtypes = [i]
         getattr(L, name).restype = None
     for name in ("quamba_debug_gemm_kind", "quamba_debug_xfmt_column_tiles"):
@@ -770,6 +771,10 @@ def quamba_debug_set_decode_stack(v):
 
 def quamba_debug_set_linear_variant(v):
     lib().quamba_debug_set_linear_variant(int(v))
+
+
+def quamba_debug_set_linattn_blocks(v):
+    lib().quamba_debug_set_linattn_blocks(int(v))
 
 
 def quamba_debug_gemm_kind(M, N, K) -> int:

@@ -1,5 +1,6 @@
 // Linear attention with a decay per head:  S_t = a_t S_{t-1} + k_t v_t^T,  o_t = scale q_t^T S_t,  a_t = exp(min(g_t, 0)),
 // S [dk, dv] in fp32 per sequence and value head.
+#include <atomic>
 #include <climits>
 #include <type_traits>
 
@@ -121,9 +122,8 @@ constexpr int kBlock = 64;
 
 struct SegArgs {
   int segments, blocks;  // of a sequence; blocks of a segment
-  int pair0, pairs;      // (sequence, value head) pairs b Hv + h of this launch
-  float *slots;          // [pairs][segments][dk][dv]: a segment's own sum of updates at slot + 1, later the state it starts from
-  float2 *decays;        // [pairs][segments]: a segment's whole decay, fp32 and what that rounding left over
+  float *slots;          // [Bt Hv][segments][dk][dv]: a segment's own sum of updates one slot on, later the state it starts from
+  float2 *decays;        // [Bt Hv][segments]: a segment's whole decay, fp32 and what that rounding left over
 };
 
 struct GTable {  // of a block's 64 tokens
@@ -201,11 +201,14 @@ __device__ __forceinline__ void make_table(float g, float scale, double carry, i
   }
 }
 
-// LDS rows of 32 KT elements whose 16-byte chunks are exchanged so that 16 rows at one chunk, and 8 rows (0-7 or 8-15) at two
-// adjacent chunks (the transposing reads), fall on different banks.  The exchange depends on the row modulo 16 only.
+// LDS rows of 32 KT elements whose 16-byte chunks are exchanged so that nothing meets on a bank that is read at once: 16 rows at
+// one chunk in 8-byte pieces; 8 rows (0-7 or 8-15) at two adjacent chunks (the transposing reads); and of 16-byte reads, whose
+// quarters are lanes 0-3, 12-15, 20-27 and so on, rows 0-3 and 12-15 at one chunk with rows 4-11 at the chunk next to it (with rows
+// r and r + 8 exchanged alike those met two at a time).  The exchange depends on the row modulo 16 only.
 template <int KT>
 __device__ __forceinline__ int swap_of(int row) {
-  return KT == 2 ? (((row >> 1) & 3) << 1) | ((row >> 3) & 1) : ((row & 7) << 1) | ((row >> 3) & 1);
+  const int high = (row >> 3) & 1;
+  return KT == 2 ? ((((row >> 1) & 3) ^ (high << 1)) << 1) | high : (((row & 7) ^ (high << 2)) << 1) | high;
 }
 template <int KT>
 __device__ __forceinline__ int tile_at(int row, int chunk) {
@@ -335,7 +338,7 @@ __device__ __forceinline__ void block_barrier() {
 // heads start on 16 bytes and a block's rows span less than 2^31 bytes: tiles travel by direct-to-LDS buffer loads, whose lanes
 // behind the end or behind dk or dv get an offset past the buffer and leave zeros.  Otherwise they pass through registers.
 //
-// LDS for two workgroups on a CU (KT = 4, NT = 2: 78.5 of 80 KB): k twice, the next block's arriving while this one's is used; q
+// LDS for two workgroups on a CU (KT = 4, NT = 2: 78.2 of 80 KB): k twice, the next block's arriving while this one's is used; q
 // and v once: q is done with at the barrier behind the weights, v belongs to one wave and is done with once it is in registers.
 template <typename T, int KT, int NT, bool OUT, bool WIDE>
 __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_kernel(LinAttnArgs a, SegArgs sg) {
@@ -354,7 +357,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
   const int id = (int)blockIdx.x < (per << 3) ? ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
   const int parts = (a.dv + 64 * NT - 1) / (64 * NT);
   const int part = id % parts, rest = id / parts;
-  const int slot = rest % sg.pairs, seg = rest / sg.pairs, pair = sg.pair0 + slot;
+  const int pairs = a.Bt * a.Hv, pair = rest % pairs, seg = rest / pairs;
   const int h = pair % a.Hv, b = pair / a.Hv, hk = h / (a.Hv / a.Hk);
   const int len = seq_len(a, b);
   const int t_lo = seg * sg.blocks * kBlock, t_hi = min(len, t_lo + sg.blocks * kBlock);
@@ -440,7 +443,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 
   // S[m][n]: rows 16 m + 4 g + r of column col0 + 16 n + c
   v4f S[2 * KT][NT];
-  const float *from = !OUT ? nullptr : (sg.segments > 1 ? sg.slots + ((size_t)slot * sg.segments + seg) * a.dk * a.dv
+  const float *from = !OUT ? nullptr : (sg.segments > 1 ? sg.slots + ((size_t)pair * sg.segments + seg) * a.dk * a.dv
                                                         : (a.state ? a.state + (size_t)pair * a.dk * a.dv : nullptr));
 #pragma unroll
   for (int m = 0; m < 2 * KT; ++m)
@@ -766,10 +769,10 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
   if constexpr (!OUT) {
     if (part == 0 && tid == 0) {
       const double dec = resets ? 0.0 : exp2_neg(G);
-      sg.decays[(size_t)slot * sg.segments + seg] = make_float2((float)dec, (float)(dec - (double)(float)dec));
+      sg.decays[(size_t)pair * sg.segments + seg] = make_float2((float)dec, (float)(dec - (double)(float)dec));
     }
   }
-  float *to = !OUT ? sg.slots + ((size_t)slot * sg.segments + seg + 1) * a.dk * a.dv
+  float *to = !OUT ? sg.slots + ((size_t)pair * sg.segments + seg + 1) * a.dk * a.dv
                    : (a.state && t_hi == len ? a.state + (size_t)pair * a.dk * a.dv : nullptr);
   if (to)
 #pragma unroll
@@ -783,66 +786,107 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
         }
 }
 
-// The segments' sums of updates joined: slot j becomes the state segment j starts from.  A thread takes one element through all of them.
+// The segments' sums of updates joined: slot j becomes the state segment j starts from.  A thread takes V elements through all
+// segments, eight of them asked for at a time: the sums wait for one another, the reads need not.
+template <int V>
 __global__ __launch_bounds__(256) void linattn_join_kernel(LinAttnArgs a, SegArgs sg) {
-  const size_t n = (size_t)a.dk * a.dv, i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const int slot = blockIdx.y, pair = sg.pair0 + slot, b = pair / a.Hv;
-  if (i >= n) return;
+  typedef float vf __attribute__((ext_vector_type(V)));
+  constexpr int U = 8;
+  const size_t n = (size_t)a.dk * a.dv, i = ((size_t)blockIdx.x * 256 + threadIdx.x) * V;
+  const int pair = blockIdx.y, b = pair / a.Hv;
+  if (i >= n) return;  // V = 4: n is a multiple of 4
   const int span = sg.blocks * kBlock, used = (seq_len(a, b) + span - 1) / span;
   if (used == 0) return;
-  float *p = sg.slots + (size_t)slot * sg.segments * n + i;
-  const float2 *d = sg.decays + (size_t)slot * sg.segments;
-  float s = a.state ? a.state[(size_t)pair * n + i] : 0.f;
-  p[0] = s;
-  for (int j = 0; j + 1 < used; ++j) {
-    const float2 f = d[j];
-    s = fmaf(s, f.x, fmaf(s, f.y, p[(size_t)(j + 1) * n]));
-    p[(size_t)(j + 1) * n] = s;
+  float *p = sg.slots + (size_t)pair * sg.segments * n + i;
+  const float2 *d = sg.decays + (size_t)pair * sg.segments;
+  vf s = vf(0.f);
+  if (a.state) s = *reinterpret_cast<const vf *>(a.state + (size_t)pair * n + i);
+  *reinterpret_cast<vf *>(p) = s;
+  for (int j0 = 1; j0 < used; j0 += U) {
+    vf u[U];
+    float2 f[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (j0 + j < used) {
+        u[j] = *reinterpret_cast<const vf *>(p + (size_t)(j0 + j) * n);
+        f[j] = d[j0 + j - 1];
+      }
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (j0 + j < used) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] = fmaf(s[e], f[j].x, fmaf(s[e], f[j].y, u[j][e]));
+        *reinterpret_cast<vf *>(p + (size_t)(j0 + j) * n) = s;
+      }
   }
 }
 
+std::atomic<int> g_segment_blocks{0};  // tuning hook
+
 struct AttnPlan {
-  int kt, nt, segments, blocks, group;  // pairs of one launch
+  int kt, nt, segments, blocks;
 };
 
+// How many segments a sequence is cut into: the cheapest by a cost in us fitted to measured times.  One segment is one launch of
+// about 5 and 0.72 c a block; more are three launches, 9, whose two passes together take c a block and 3 to start, 1.42 times that
+// with two workgroups on a CU, plus the sums' way through memory and the chain that joins them.  At 32 shapes (1 to 80 heads, 128
+// to 65536 tokens, dk 32 to 256) the choice is within 10 % of the best of up to 16 that were timed: 1 x 2048, 80 heads of 128 x 64,
+// 6 blocks a segment 58 us, 4 66, 8 67, all in one 115; 8 x 256, 16 heads of 64 x 64, all in one 15.5, 2 blocks 21.5, single ones
+// 23.7; 1 x 16384, one head of 64 x 64, 3 blocks 33, single ones 44, all in one 617.
 AttnPlan plan_prefill(int Bt, int L, int Hv, int dk, int dv) {
-  AttnPlan p{2, 1, 1, 1, 1};
+  AttnPlan p{2, 1, 1, 1};
   if (Bt == 0 || L == 0) return p;
   p.kt = dk <= 64 ? 2 : (dk <= 128 ? 4 : 8);
   p.nt = dv > 64 && p.kt < 8 ? 2 : 1;
-  const long long parts = (dv + 64 * p.nt - 1) / (64 * p.nt), pairs = (long long)Bt * Hv, blocks = (L + kBlock - 1LL) / kBlock;
-  p.group = (int)pairs;
-  long long segments = 512 / (pairs * parts);
-  if (segments > blocks) segments = blocks;
-  if (segments < 1) segments = 1;
-  p.blocks = (int)((blocks + segments - 1) / segments);
-  p.segments = p.blocks > 0 ? (int)((blocks + p.blocks - 1) / p.blocks) : 1;
+  const double pairs = (double)Bt * Hv, parts = (dv + 64 * p.nt - 1) / (64 * p.nt);
+  const long long blocks = (L + kBlock - 1LL) / kBlock;
+  const double c = p.kt == 8 ? 7.6 : (p.kt == 4 ? (p.nt == 2 ? 6.7 : 4.9) : (p.nt == 2 ? 4.6 : 3.4));
+  const double on_cu = p.kt == 8 ? 1 : 2, slow = p.kt == 8 ? 1.0 : 1.42;
+  auto rounds = [&](double wgs) {
+    const double full = __builtin_floor(wgs / (256 * on_cu)), rest = wgs - full * 256 * on_cu;
+    return full * slow + (rest == 0 ? 0.0 : (rest <= 256 ? 1.0 : slow));
+  };
+  double best = 5 + rounds(pairs * parts) * 0.72 * c * blocks;
+  long long at = blocks;
+  if (pairs <= 65535)
+    for (long long b = 1; b < blocks; b = b < 4 ? b + 1 : b + b / 4) {
+      const double n = (double)((blocks + b - 1) / b);
+      const double t = 9 + rounds(pairs * parts * n) * (c * b + 3) + pairs * n * dk * dv * 8.0 / 4e6 + 0.12 * n;
+      if (t < best) best = t, at = b;
+    }
+  const int forced = g_segment_blocks.load(std::memory_order_relaxed);
+  if (forced > 0 && pairs <= 65535) at = forced < blocks ? forced : blocks;
+  p.blocks = (int)at;
+  p.segments = (int)((blocks + at - 1) / at);
   return p;
 }
 
-size_t slots_bytes(const AttnPlan &p, int dk, int dv) {
-  return p.segments > 1 ? align_up((size_t)p.group * p.segments * dk * dv * sizeof(float), 256) : 0;
+size_t slots_bytes(const AttnPlan &p, int Bt, int Hv, int dk, int dv) {
+  return align_up((size_t)Bt * Hv * p.segments * dk * dv * sizeof(float), 256);
 }
-size_t prefill_workspace(const AttnPlan &p, int dk, int dv) {
-  return p.segments > 1 ? slots_bytes(p, dk, dv) + align_up((size_t)p.group * p.segments * sizeof(float2), 256) : 256;
+size_t prefill_workspace(const AttnPlan &p, int Bt, int Hv, int dk, int dv) {
+  return p.segments > 1 ? slots_bytes(p, Bt, Hv, dk, dv) + align_up((size_t)Bt * Hv * p.segments * sizeof(float2), 256) : 256;
 }
 
 template <typename T, int KT, int NT, bool WIDE>
 int run_blocks(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t st) {
-  const int parts = (a.dv + 64 * NT - 1) / (64 * NT), pairs = a.Bt * a.Hv;
-  for (int at = 0; at < pairs; at += p.group) {
-    SegArgs sg{p.segments, p.blocks, at, pairs - at < p.group ? pairs - at : p.group, static_cast<float *>(ws), nullptr};
-    sg.decays = reinterpret_cast<float2 *>(static_cast<char *>(ws) + slots_bytes(p, a.dk, a.dv));
-    const unsigned one = (unsigned)parts * sg.pairs;
-    if (p.segments > 1) {
-      hipLaunchKernelGGL((linattn_blocks_kernel<T, KT, NT, false, WIDE>), dim3(one * (p.segments - 1)), dim3(256), 0, st, a, sg);
-      QUAMBA_LAUNCH_CHECK();
-      hipLaunchKernelGGL(linattn_join_kernel, dim3((a.dk * a.dv + 255) / 256, sg.pairs), dim3(256), 0, st, a, sg);
-      QUAMBA_LAUNCH_CHECK();
-    }
-    hipLaunchKernelGGL((linattn_blocks_kernel<T, KT, NT, true, WIDE>), dim3(one * p.segments), dim3(256), 0, st, a, sg);
+  const int parts = (a.dv + 64 * NT - 1) / (64 * NT);
+  const long long one = (long long)parts * a.Bt * a.Hv;
+  if (one * p.segments > INT_MAX)
+    return fail(QUAMBA_EUNSUPPORTED, "linattn_prefill: %d sequences of %d heads are more than one launch takes", a.Bt, a.Hv);
+  SegArgs sg{p.segments, p.blocks, static_cast<float *>(ws), nullptr};
+  if (p.segments > 1) {
+    sg.decays = reinterpret_cast<float2 *>(static_cast<char *>(ws) + slots_bytes(p, a.Bt, a.Hv, a.dk, a.dv));
+    hipLaunchKernelGGL((linattn_blocks_kernel<T, KT, NT, false, WIDE>), dim3((unsigned)(one * (p.segments - 1))), dim3(256), 0, st, a, sg);
+    QUAMBA_LAUNCH_CHECK();
+    if (a.dk * a.dv % 4 == 0)
+      hipLaunchKernelGGL(linattn_join_kernel<4>, dim3((a.dk * a.dv / 4 + 255) / 256, a.Bt * a.Hv), dim3(256), 0, st, a, sg);
+    else
+      hipLaunchKernelGGL(linattn_join_kernel<1>, dim3((a.dk * a.dv + 255) / 256, a.Bt * a.Hv), dim3(256), 0, st, a, sg);
     QUAMBA_LAUNCH_CHECK();
   }
+  hipLaunchKernelGGL((linattn_blocks_kernel<T, KT, NT, true, WIDE>), dim3((unsigned)(one * p.segments)), dim3(256), 0, st, a, sg);
+  QUAMBA_LAUNCH_CHECK();
   return QUAMBA_OK;
 }
 
@@ -856,8 +900,8 @@ int run_prefill(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t s
 // Rows that the direct-to-LDS loads can take: every row and head starts on 16 bytes, 64 rows lie within 2^31 bytes.
 bool wide_rows(const LinAttnArgs &a) {
   const long long most = 1LL << 23;
-  return aligned(a.q, 16) && aligned(a.k, 16) && aligned(a.v, 16) && aligned(a.out, 8) && a.ldo % 4 == 0 && a.ldo < most && a.ldq % 8 == 0 && a.ldk % 8 == 0 && a.ldv % 8 == 0 && a.dk % 8 == 0 &&
-         a.dv % 8 == 0 && a.ldq < most && a.ldk < most && a.ldv < most;
+  return aligned(a.q, 16) && aligned(a.k, 16) && aligned(a.v, 16) && aligned(a.out, 8) && a.ldq % 8 == 0 && a.ldk % 8 == 0 &&
+         a.ldv % 8 == 0 && a.ldo % 4 == 0 && a.dk % 8 == 0 && a.dv % 8 == 0 && a.ldq < most && a.ldk < most && a.ldv < most && a.ldo < most;
 }
 
 int check(const char *what, int type, const LinAttnArgs &a) {
@@ -866,6 +910,7 @@ int check(const char *what, int type, const LinAttnArgs &a) {
     return fail(QUAMBA_EINVAL, "%s: Bt=%d L=%d Hk=%d Hv=%d dk=%d dv=%d", what, a.Bt, a.L, a.Hk, a.Hv, a.dk, a.dv);
   if (a.Hv % a.Hk) return fail(QUAMBA_EUNSUPPORTED, "%s: %d value heads are no multiple of %d key heads", what, a.Hv, a.Hk);
   if (a.dk > 256 || a.dv > 1024) return fail(QUAMBA_EUNSUPPORTED, "%s: dk=%d dv=%d (at most 256 and 1024)", what, a.dk, a.dv);
+  if (a.L > 1 << 30) return fail(QUAMBA_EUNSUPPORTED, "%s: L=%d (at most 2^30)", what, a.L);
   if (a.Bt > 65535 || a.Hv > 65535) return fail(QUAMBA_EUNSUPPORTED, "%s: Bt=%d Hv=%d (at most 65535 each)", what, a.Bt, a.Hv);
   const long long qw = (long long)a.Hk * a.dk, vw = (long long)a.Hv * a.dv;
   if (a.ldq < qw || a.ldk < qw || a.ldv < vw || a.ldo < vw || (a.g && a.ldg != 0 && a.ldg < a.Hv))
@@ -892,7 +937,7 @@ size_t quamba_linattn_workspace_bytes(int Bt, int L, int Hk, int Hv, int dk, int
     fail(QUAMBA_EINVAL, "linattn: Bt=%d L=%d Hk=%d Hv=%d dk=%d dv=%d", Bt, L, Hk, Hv, dk, dv);
     return 0;
   }
-  return prefill_workspace(plan_prefill(Bt, L, Hv, dk, dv), dk, dv);
+  return prefill_workspace(plan_prefill(Bt, L, Hv, dk, dv), Bt, Hv, dk, dv);
 }
 
 int quamba_linattn_prefill(int type, const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, const float *log_decay,
@@ -903,8 +948,8 @@ int quamba_linattn_prefill(int type, const void *q, int ldq, const void *k, int 
   if (rc != QUAMBA_OK || Bt == 0 || L == 0) return rc;
   if (ws && !aligned(ws, 256)) return fail(QUAMBA_EINVAL, "linattn_prefill: workspace must be 256-byte aligned");
   const AttnPlan p = plan_prefill(Bt, L, Hv, dk, dv);
-  if (p.segments > 1 && (!ws || ws_bytes < prefill_workspace(p, dk, dv)))
-    return fail(QUAMBA_EWORKSPACE, "linattn_prefill: workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, prefill_workspace(p, dk, dv));
+  if (p.segments > 1 && (!ws || ws_bytes < prefill_workspace(p, Bt, Hv, dk, dv)))
+    return fail(QUAMBA_EWORKSPACE, "linattn_prefill: workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, prefill_workspace(p, Bt, Hv, dk, dv));
   hipStream_t st = as_stream(stream);
   if (type == QUAMBA_TYPE_F16) return wide_rows(a) ? run_prefill<_Float16, true>(a, p, ws, st) : run_prefill<_Float16, false>(a, p, ws, st);
   return wide_rows(a) ? run_prefill<__bf16, true>(a, p, ws, st) : run_prefill<__bf16, false>(a, p, ws, st);
@@ -922,3 +967,5 @@ int quamba_linattn_step(int type, const void *q, int ldq, const void *k, int ldk
 }
 
 }  // extern "C"
+
+extern "C" void quamba_debug_set_linattn_blocks(int v) { quamba::g_segment_blocks.store(v); }

@@ -78,3 +78,19 @@ def test_workspace_queries():
     assert Q.quamba_linattn_workspace_bytes(1, 2048, 1, 80, 128, 64) > 0 and Q.quamba_linattn_workspace_bytes(0, 0, 1, 1, 1, 1) > 0
     assert Q.quamba_linear_workspace_bytes(1, 0, 1) == 0 and "N=0" in Q.quamba_last_error()
     assert Q.quamba_linattn_workspace_bytes(1, 1, 1, 1, 0, 1) == 0 and "dk=0" in Q.quamba_last_error()
+
+
+def test_linattn_prefill_refuses_prompts_past_its_counters_and_a_short_workspace():
+    _refused(Q.quamba_linattn_prefill, {**PREFILL, "L": 2 ** 30 + 1}, UNSUPPORTED, "at most 2^30")
+    Q.quamba_debug_set_linattn_blocks(1)  # two segments: their sums need room
+    try:
+        assert Q.quamba_linattn_workspace_bytes(1, 100, 1, 1, 16, 16) >= 2 * 16 * 16 * 4
+        _refused(Q.quamba_linattn_prefill, {**PREFILL, "Bt": 1, "L": 100, "ws": None}, WORKSPACE, "workspace of 0 bytes")
+    finally:
+        Q.quamba_debug_set_linattn_blocks(0)
+
+
+def test_linattn_prefill_refuses_more_heads_than_a_launch_takes():
+    n = 65535
+    _refused(Q.quamba_linattn_prefill, {**PREFILL, "Bt": n, "L": 1, "Hk": n, "Hv": n, "dk": 1, "dv": 1, "ldq": n, "ldk": n, "ldv": n, "ldg": n, "ldo": n},
+             UNSUPPORTED, "more than one launch")
