@@ -647,6 +647,7 @@ int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int 
                hipStream_t st) {
   if (((M + 31LL) / 32) * ((N + 31LL) / 32) > INT_MAX)
     return fail(QUAMBA_EUNSUPPORTED, "linear: %d x %d outputs are more than one launch takes", M, N);
+  if (M > 1 << 30 || N > 1 << 30 || K > 1 << 30) return fail(QUAMBA_EUNSUPPORTED, "linear: M=%d N=%d K=%d (at most 2^30 each)", M, N, K);
   bool wx = rows_wide(x, ldx, K), ww = rows_wide(W, ldw, K);
   if (copies(M) && !(wx && ww) && ws && (wx ? 0 : aligned_bytes(M, K)) + (ww ? 0 : aligned_bytes(N, K)) <= ws_bytes &&
       g_linear_variant.load(std::memory_order_relaxed) < 0) {

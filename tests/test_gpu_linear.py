@@ -174,3 +174,21 @@ def test_an_empty_call_touches_nothing():
     out = torch.full((4, 8), 3.0, dtype=torch.float16, device=DEV)
     Q.quamba_linear(Q.TYPE_F16, out, 8, out, 8, None, None, 0, 0, 8, 8, Q.ACT_NONE, Q.TYPE_F16, out, 8, None)
     assert (out == 3.0).all()
+
+
+@pytest.fixture
+def forced():
+    yield Q.quamba_debug_set_linear_variant
+    Q.quamba_debug_set_linear_variant(-1)
+
+
+@pytest.mark.parametrize("variant", range(12))
+def test_every_kernel_at_every_size_it_takes(variant, forced):
+    """Also where the rule would not take it: fewer rows than a tile, one slice of K, K groups that have nothing to do."""
+    forced(variant)
+    for n, (M, N, K) in enumerate([(1, 70, 72), (2, 33, 8), (4, 33, 70), (16, 130, 264), (65, 200, 320), (300, 330, 136), (513, 640, 1288)]):
+        dt = (torch.float16, torch.bfloat16)[n & 1]
+        x, W, b, r = _inputs(M, N, K, dt, dt, True, True)
+        want, tol = _bound(x, W, b, r, "silu", dt)
+        got = _f64(_run(x, W, b, r, "silu", dt))
+        assert (np.abs(got - want) <= tol).all(), (M, N, K, (np.abs(got - want) / tol).max())

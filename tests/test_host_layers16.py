@@ -94,3 +94,8 @@ def test_linattn_prefill_refuses_more_heads_than_a_launch_takes():
     n = 65535
     _refused(Q.quamba_linattn_prefill, {**PREFILL, "Bt": n, "L": 1, "Hk": n, "Hv": n, "dk": 1, "dv": 1, "ldq": n, "ldk": n, "ldv": n, "ldg": n, "ldo": n},
              UNSUPPORTED, "more than one launch")
+
+
+@pytest.mark.parametrize("change", [dict(M=2 ** 30 + 1), dict(N=2 ** 30 + 1, ldo=2 ** 31 - 1), dict(K=2 ** 30 + 1, ldx=2 ** 31 - 1, ldw=2 ** 31 - 1)])
+def test_linear_refuses_sizes_past_its_counters(change):
+    _refused(Q.quamba_linear, {**LINEAR, **change}, UNSUPPORTED, "at most 2^30")
