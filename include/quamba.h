@@ -610,6 +610,8 @@ int quamba_linear(int type, const void *x, int ldx, const void *W, int ldw, cons
  * [0, L]; tokens behind it are not read, their output rows are left as they were, and an empty sequence keeps its state.  The sums are
  * taken block by block: the result is that of the recurrence up to the rounding of fp32 sums (block weights carry 16 bits or more,
  * the state's update 22 or more).  Workspace: quamba_linattn_workspace_bytes, 256-byte aligned.
+ * Infinities and NaN stay out of everything before their token: one in v makes its column of outputs and state NaN or infinite
+ * from its token on, one in k or g its head's; a reset does not clear a state that holds one.
  * quamba_linattn_step is one token of every sequence (L = 1, state required), strides between sequences.
  * out must not overlap an input, state no other buffer.  Bt = 0 or L = 0 does nothing. */
 size_t quamba_linattn_workspace_bytes(int Bt, int L, int Hk, int Hv, int dk, int dv);

@@ -1,6 +1,7 @@
 // Linear attention with a decay per head:  S_t = a_t S_{t-1} + k_t v_t^T,  o_t = scale q_t^T S_t,  a_t = exp(min(g_t, 0)),
 // S [dk, dv] in fp32 per sequence and value head.
 #include <atomic>
+#include <cfloat>
 #include <climits>
 #include <type_traits>
 
@@ -287,6 +288,15 @@ __device__ __forceinline__ float max_over_groups(float m) {
   return fmaxf(m, __shfl_xor(m, 32));
 }
 
+// acc + 0 w.x + 0 w.y of two 16-bit values: NaN once one of them is infinite or NaN
+__device__ __forceinline__ float times_zero(unsigned w, float acc, __bf16) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, w), __builtin_bit_cast(b2, 0u), acc, false);
+}
+__device__ __forceinline__ float times_zero(unsigned w, float acc, _Float16) {
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w), __builtin_bit_cast(h2, 0u), acc, false);
+}
 __device__ __forceinline__ int seq_len(const LinAttnArgs &a, int b) { return a.lens ? min(max(a.lens[b], 0), a.L) : a.L; }
 
 // Two fp32 values as one word of 16-bit ones, rounded to nearest
@@ -637,7 +647,52 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
         for (int n = 0; n < NT; ++n) asm volatile("" : "+v"(fv[kb][n])::"memory");  // read before the next block's may arrive
       if constexpr (!SPREAD) fetch_v(t1);
     }
+    bool any = false;
     if constexpr (OUT) {
+      b8 ph[2][2], pl[2][2];
+      auto ask_p = [&](int tb) {
+#pragma unroll
+        for (int kb = 0; kb <= tb / 2; ++kb) {
+          ph[tb & 1][kb] = weight_operand(lp, 16 * tb + c, kb, lane);
+          pl[tb & 1][kb] = weight_operand(lpl, 16 * tb + c, kb, lane);
+        }
+      };
+      ask_p(0);
+      // A token's NaN or infinity in v must not reach earlier outputs, and in a product it would: its weight there is 0.  Where a
+      // wave finds one (rare; looking for it costs 1 %) it leaves them out of the product, and the outputs of their column are NaN from
+      // the first's token on.
+      float bad[2] = {0.f, 0.f};
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) bad[e & 1] = times_zero(__builtin_bit_cast(u4, fv[kb][n])[e], bad[e & 1], T());
+      any = __ballot(!(bad[0] + bad[1] == 0.f)) != 0;
+      if (__builtin_expect(any, 0)) {
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          int first = kBlock;
+#pragma unroll
+          for (int kb = 1; kb >= 0; --kb)
+#pragma unroll
+            for (int e = 7; e >= 0; --e)
+              if (!(fabsf(to_f32(fv[kb][n][e])) <= FLT_MAX)) {
+                first = 32 * kb + 16 * (e >> 2) + 4 * g + (e & 3);
+                fv[kb][n][e] = T(0.f);
+              }
+          first = min(first, __shfl_xor(first, 16));
+          first = min(first, __shfl_xor(first, 32));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int of = __shfl(first, 4 * g + r);
+#pragma unroll
+            for (int tb = 0; tb < 4; ++tb)
+              if (16 * tb + c >= of) O[tb][n][r] = __builtin_nanf("");
+          }
+        }
+      }
       b8 vh[2][NT], vl[F16 ? 2 : 1][F16 ? NT : 1];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -653,15 +708,6 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
             vh[kb][n] = fv[kb][n];
           }
         }
-      b8 ph[2][2], pl[2][2];
-      auto ask_p = [&](int tb) {
-#pragma unroll
-        for (int kb = 0; kb <= tb / 2; ++kb) {
-          ph[tb & 1][kb] = weight_operand(lp, 16 * tb + c, kb, lane);
-          pl[tb & 1][kb] = weight_operand(lpl, 16 * tb + c, kb, lane);
-        }
-      };
-      ask_p(0);
 #pragma unroll
       for (int tb = 0; tb < 4; ++tb) {
         if (tb < 3) ask_p(tb + 1);
@@ -697,7 +743,15 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
       }
     }
 
-    // the state's update: decay, then k (weighted v)^T
+    // the state's update: decay, then k (weighted v)^T, with v as it is
+    if constexpr (OUT)
+      if (__builtin_expect(any, 0)) {
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) fv[kb][n] = value_operand<T, NT>(lv, kb, n, lane);
+      }
     constexpr int VP = F16 ? 2 : 3;
     u4 wv[VP][2][NT];
     float back[NT];

@@ -232,3 +232,73 @@ def test_empty_calls_touch_nothing():
     Q.quamba_linattn_prefill(Q.TYPE_F16, c.rows, 48, c.rows, 48, c.rows, 48, None, 0, None, 1, 0, 1, 1, 16, 16, 1.0, c.out, 16, c.state, None)
     Q.quamba_linattn_step(Q.TYPE_F16, c.rows, 48, c.rows, 48, c.rows, 48, None, 0, 0, 1, 1, 16, 16, 1.0, c.out, 16, c.state)
     assert torch.equal(c.state, before) and (c.out == 7.0).all()
+
+
+@pytest.fixture
+def segments():
+    yield Q.quamba_debug_set_linattn_blocks
+    Q.quamba_debug_set_linattn_blocks(0)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("blocks", [1, 2, 3, 100])
+def test_any_number_of_segments(blocks, dt, segments):
+    segments(blocks)
+    for shape in ((2, 150, 1, 2, 64, 64), (1, 700, 2, 4, 128, 64), (3, 300, 1, 1, 40, 130), (1, 260, 1, 1, 200, 72), (2, 190, 1, 1, 33, 19)):
+        for decay in ("token", "strong", "reset"):
+            c = Call(*shape, dt, decay=decay, state=decay != "strong")
+            want = c.want()
+            c.prefill()
+            c.check(want)
+    c = Call(6, 200, 1, 3, 96, 80, dt)
+    c.lens = torch.tensor([200, 0, 1, 64, 65, 129], dtype=torch.int32, device=DEV)
+    for b, n in enumerate(c.lens.tolist()):
+        c.rows[b, n:] = float("nan")
+        c.g[b, n:] = float("nan")
+    want = c.want()
+    c.prefill()
+    c.check(want)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("shape, token", [((2, 150, 1, 2, 64, 64), 40), ((1, 300, 1, 2, 128, 64), 64), ((1, 130, 2, 2, 128, 128), 63),
+                                          ((1, 200, 1, 1, 256, 80), 100), ((1, 100, 1, 2, 33, 19), 0), ((1, 90, 1, 1, 24, 130), 89)])
+def test_a_bad_token_stays_out_of_earlier_outputs(shape, token, dt):
+    """NaN or an infinity in v reaches its own column from its token on, in k or the decay its own head from its token on."""
+    clean = Call(*shape, dt)
+    clean.prefill()
+    B, L, Hk, Hv, dk, dv = shape
+    view = lambda c: (c.out.view(B, L, Hv, dv), c.state)
+    want, want_state = view(clean)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        c = Call(*shape, dt)
+        c.rows[0, token, 2 * Hk * dk + dv // 2] = value
+        c.prefill()
+        got, state = view(c)
+        hit = torch.zeros((B, L, Hv, dv), dtype=torch.bool, device=DEV)
+        hit[0, token:, 0, dv // 2] = True
+        assert torch.equal(got[~hit], want[~hit]) and not torch.isfinite(got[hit]).any()
+        hit = torch.zeros_like(state, dtype=torch.bool)
+        hit[0, 0, :, dv // 2] = True
+        assert torch.equal(state[~hit], want_state[~hit]) and not torch.isfinite(state[hit]).any()
+    for where in ("k", "decay"):
+        c = Call(*shape, dt)
+        if where == "k":
+            c.rows[0, token, Hk * dk] = float("nan")
+        else:
+            c.g[0, token, 0] = float("nan")
+        c.prefill()
+        got, state = view(c)
+        heads = Hv // Hk if where == "k" else 1
+        hit = torch.zeros((B, L, Hv, dv), dtype=torch.bool, device=DEV)
+        hit[0, token:, :heads] = True
+        assert torch.equal(got[~hit], want[~hit]) and torch.isnan(got[hit]).all()
+
+
+@pytest.mark.parametrize("L, ld", [(2100, 1 << 20), (260, (1 << 23) + 8)])
+def test_offsets_past_32_bits(L, ld):
+    """The last tokens start more than 2^31 elements in; in the second case a block of tokens spans more than 2^31 bytes."""
+    c = Call(1, L, 1, 1, 64, 64, torch.bfloat16, pad=ld - 192)
+    want = c.want()
+    c.prefill()
+    c.check(want)
