@@ -334,6 +334,34 @@ __device__ __forceinline__ void tile_load(const void *base, int off, int soff, c
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(off), "s"(rsrc), "s"(soff));
 }
 
+// Eight elements of a row of K from element k on, zeros behind K and where the row is off, in two steps: what is in flight is 16
+// bytes that end with the row at the latest, and they are moved into place when they are used.  With the last elements loaded one
+// by one every load waited for its own (10 x 570, 29 heads of 85 x 176: 443 -> 338 us).
+template <typename T>
+__device__ __forceinline__ typename Half<T>::v8 ask8(const T *row, int k, int K) {
+  typename Half<T>::v8 v = {};
+  if (K >= 8) {
+    __builtin_memcpy(&v, row + min(k, K - 8), 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = k == 0 && e < K ? row[min(e, K - 1)] : static_cast<T>(0.f);
+  }
+  return v;
+}
+template <typename V8>
+__device__ __forceinline__ V8 place8(V8 v, int k, int K, bool on) {
+  typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
+  u64x2 w = __builtin_bit_cast(u64x2, v);
+  if (K & 7) {  // the last elements of a row stand at the end of what was loaded
+    const int bits = K < 8 ? 0 : 16 * max(k - (K - 8), 0), part = bits & 63;
+    const unsigned long long lo = bits & 64 ? w[1] : w[0], hi = bits & 64 ? 0 : w[1];
+    w[0] = (lo >> part) | (part ? hi << (64 - part) : 0);
+    w[1] = hi >> part;
+  }
+  if (!on || k >= K) w = u64x2{0, 0};
+  return __builtin_bit_cast(V8, w);
+}
+
 // Order LDS accesses (the compiler's and the wave's own) around the hardware barrier.  VM: so many of the wave's vector memory
 // operations, the youngest, may still be under way (they complete in the order of issue); 63: all.
 template <int VM>
@@ -404,14 +432,13 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
     ov = col0 + v_chunk * 8 < a.dv ? (int)(v_row * a.ldv + col0 + v_chunk * 8) * 2 : OFF;
   }
   v8 rq[!WIDE && OUT ? NL : 1], rk[!WIDE ? NL : 1], rv[!WIDE ? NLV : 1];
-  const v8 zero = {};
   auto load_tile = [&](const T *p, long long ld, const int (&o)[PH], v8 *r, int t0, char *tile, int i) {  // load i of the wave's NL
     const int n = t_hi - t0;  // rows that count
     if constexpr (WIDE) {
       const int off = n >= kBlock || tile_row(i) < n ? o[i % PH] : OFF;
       tile_load(p + (size_t)t0 * ld, off, (int)((i / PH) * (PH * 4 * RPL) * ld * 2), tile + ((i / PH) * PH * 4 + (i % PH) * 4 + wave) * 1024);
     } else {
-      r[i] = tile_row(i) < n ? row8(p + (size_t)(t0 + tile_row(i)) * ld, tile_chunk(i) * 8, a.dk) : zero;
+      r[i] = ask8(p + (size_t)(t0 + min(tile_row(i), n - 1)) * ld, tile_chunk(i) * 8, a.dk);
     }
   };
   auto load_v = [&](int t0, int i) {  // of NLV
@@ -419,7 +446,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
     if constexpr (WIDE)
       tile_load(pv + (size_t)t0 * a.ldv, n >= kBlock || row < n ? ov : OFF, (int)(RPLV * i * a.ldv * 2), lv + i * 1024);
     else
-      rv[i] = row < n ? row8(pv + (size_t)(t0 + row) * a.ldv, col0 + v_chunk * 8, a.dv) : zero;
+      rv[i] = ask8(pv + (size_t)(t0 + min(row, n - 1)) * a.ldv, col0 + v_chunk * 8, a.dv);
   };
   auto fetch_tile = [&](const T *p, long long ld, const int (&o)[PH], v8 *r, int t0, char *tile) {
 #pragma unroll
@@ -429,16 +456,19 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 #pragma unroll
     for (int i = 0; i < NLV; ++i) load_v(t0, i);
   };
-  auto park = [&](char *lk) {  // what came through registers
+  auto park = [&](char *lk, int t0) {  // what came through registers
     if constexpr (!WIDE) {
+      const int n = t_hi - t0;
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int at = ((i / PH) * PH * 4 + (i % PH) * 4 + wave) * 1024 + lane * 16;
-        if constexpr (OUT) *reinterpret_cast<v8 *>(lq + at) = rq[i];
-        *reinterpret_cast<v8 *>(lk + at) = rk[i];
+        const bool on = tile_row(i) < n;
+        if constexpr (OUT) *reinterpret_cast<v8 *>(lq + at) = place8(rq[i], tile_chunk(i) * 8, a.dk, on);
+        *reinterpret_cast<v8 *>(lk + at) = place8(rk[i], tile_chunk(i) * 8, a.dk, on);
       }
 #pragma unroll
-      for (int i = 0; i < NLV; ++i) *reinterpret_cast<v8 *>(lv + i * 1024 + lane * 16) = rv[i];
+      for (int i = 0; i < NLV; ++i)
+        *reinterpret_cast<v8 *>(lv + i * 1024 + lane * 16) = place8(rv[i], col0 + v_chunk * 8, a.dv, v_row + RPLV * i < n);
     }
   };
   auto log_decay = [&](int t0) {
@@ -475,7 +505,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
   double G = 0.0;  // of the segment
   int resets = 0;
   if (wave == 0) make_table(gt, a.scale, 1.0, lane, tables[0]);
-  park(lks);
+  park(lks, t_lo);
   block_barrier<0>();
 
   int buf = 0;
@@ -735,9 +765,15 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
                                                   (int)(16 * tb * a.ldo * 2), 0);
           } else if (t < t_hi) {
             const int col = col0 + 16 * n + 4 * g;
+            T *to = po + (size_t)t * a.ldo + col;
+            if (col + 4 <= a.dv) {
+              const unsigned w[2] = {pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+              __builtin_memcpy(to, w, 8);
+            } else {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (col + r < a.dv) po[(size_t)t * a.ldo + col + r] = from_f32<T>(o[r]);
+              for (int r = 0; r < 3; ++r)
+                if (col + r < a.dv) to[r] = from_f32<T>(o[r]);
+            }
           }
         }
       }
@@ -814,7 +850,7 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[i][n][r] = F16 ? fmaf(u[n][r], back[n], S[i][n][r] * dec) : u[n][r];
     }
-    if (more) park(lk_next);
+    if (more) park(lk_next, t1);
     // The next block's k and q are in LDS (where one of their loads is under way the NLV v loads behind it are too), this one's are
     // done with.
     block_barrier<SPREAD ? NLV : 0>();
@@ -944,11 +980,14 @@ int run_blocks(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t st
   return QUAMBA_OK;
 }
 
+// Rows that pass through registers leave too few of them for two column tiles a wave at KT = 4 (10 x 570, 29 heads of 85 x 176:
+// 135 us with one, 338 with two).
 template <typename T, bool WIDE>
 int run_prefill(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t st) {
   if (p.kt == 2) return p.nt == 1 ? run_blocks<T, 2, 1, WIDE>(a, p, ws, st) : run_blocks<T, 2, 2, WIDE>(a, p, ws, st);
-  if (p.kt == 4) return p.nt == 1 ? run_blocks<T, 4, 1, WIDE>(a, p, ws, st) : run_blocks<T, 4, 2, WIDE>(a, p, ws, st);
-  return run_blocks<T, 8, 1, WIDE>(a, p, ws, st);
+  if constexpr (WIDE)
+    if (p.kt == 4 && p.nt == 2) return run_blocks<T, 4, 2, WIDE>(a, p, ws, st);
+  return p.kt == 4 ? run_blocks<T, 4, 1, WIDE>(a, p, ws, st) : run_blocks<T, 8, 1, WIDE>(a, p, ws, st);
 }
 
 // Rows that the direct-to-LDS loads can take: every row and head starts on 16 bytes, 64 rows lie within 2^31 bytes.
