@@ -786,7 +786,10 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) fv[kb][n] = value_operand<T, NT>(lv, kb, n, lane);
+          for (int n = 0; n < NT; ++n) {
+            fv[kb][n] = value_operand<T, NT>(lv, kb, n, lane);
+            asm volatile("" : "+v"(fv[kb][n])::"memory");  // before the next block's may arrive
+          }
       }
     constexpr int VP = F16 ? 2 : 3;
     u4 wv[VP][2][NT];
