@@ -656,7 +656,7 @@ int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int 
     if (rc == QUAMBA_OK && !ww) rc = align_rows(&W, &ldw, N, K, &at, st);
     if (rc != QUAMBA_OK) return rc;
     wx = ww = true;
-    K = (int)align_up(K, kCopyUnit);
+    K = (int)align_up(K, 8);  // no further: the other operand may not be a copy, and what stands behind its K is not zero
   }
   switch (plan_linear(M, N, K, wx && ww)) {
     case 0: return run_any<T, O, 1, 1>(x, ldx, W, ldw, M, N, K, epi, st);

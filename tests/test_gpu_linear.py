@@ -192,3 +192,20 @@ def test_every_kernel_at_every_size_it_takes(variant, forced):
         want, tol = _bound(x, W, b, r, "silu", dt)
         got = _f64(_run(x, W, b, r, "silu", dt))
         assert (np.abs(got - want) <= tol).all(), (M, N, K, (np.abs(got - want) / tol).max())
+
+
+@pytest.mark.parametrize("M, N, K", [(40, 90, 72), (300, 300, 136), (700, 640, 8)])
+def test_one_operand_copied_the_other_not(M, N, K):
+    """One operand's rows start on 16 bytes, the other's do not; what stands behind the rows of both is NaN."""
+    dt = torch.bfloat16
+    for x_shift, w_shift in ((0, 1), (1, 0)):
+        def view(rows, shift, std):
+            flat = torch.full((rows * (K + 56) + shift,), float("nan"), dtype=dt, device=DEV)
+            v = flat[shift:].view(rows, K + 56)[:, :K]
+            v.copy_(torch.randn((rows, K), generator=torch.Generator(device=DEV).manual_seed(rows + shift), device=DEV) * std)
+            return v
+
+        x, W = view(M, x_shift, 1.0), view(N, w_shift, 2 * K ** -0.5)
+        want, tol = _bound(x, W, None, None, "none", dt)
+        got = _f64(_run(x, W, None, None, "none", dt, ws=_ws(M, N, K)))
+        assert (np.abs(got - want) <= tol).all()
