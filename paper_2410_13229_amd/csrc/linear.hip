@@ -542,14 +542,24 @@ __global__ __launch_bounds__(256) void linear_vec_kernel(const T *__restrict__ x
     put1<O>(epi, one, gm, gn, LANES == 64 ? part[wave][mine] : part[0][mine] + part[1][mine] + part[2][mine] + part[3][mine]);
 }
 
-// Rows of any alignment copied to rows of a multiple of 64 elements, zeros behind K.
+// Rows of any alignment copied to rows of a multiple of 64 elements, zeros behind K: both operands in one launch (or one of them:
+// the other has no chunks).  A division of 64 bits is as long as the copy, so only what needs one does it.
 template <typename T>
-__global__ __launch_bounds__(256) void align_rows_kernel(const T *__restrict__ x, long long ldx, long long chunks, int per_row, int K, T *__restrict__ out) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= chunks) return;
-  const long long row = i / per_row;
+struct RowCopy {
+  const T *from;
+  long long ld, chunks;  // of 8 elements
+  T *to;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void align_rows_kernel(RowCopy<T> a, RowCopy<T> b, int per_row, int K) {
+  long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const bool second = i >= a.chunks;
+  if (second) i -= a.chunks;
+  const RowCopy<T> &c = second ? b : a;
+  if (i >= c.chunks) return;
+  const long long row = a.chunks + b.chunks <= INT_MAX ? (long long)((unsigned)i / (unsigned)per_row) : i / per_row;
   const int k = (int)(i - row * per_row) * 8;
-  *reinterpret_cast<typename Half<T>::v8 *>(out + i * 8) = row8(x + row * ldx, k, K);
+  *reinterpret_cast<typename Half<T>::v8 *>(c.to + i * 8) = row8(c.from + row * c.ld, k, K);
 }
 
 std::atomic<int> g_linear_variant{-1};
@@ -629,19 +639,6 @@ size_t aligned_bytes(int rows, int K) { return align_up((size_t)rows * align_up(
 // More rows than the streaming kernels take: operands of any alignment are worth copying to 16-byte rows first
 bool copies(int M) { return M > 16; }
 
-template <typename T>
-int align_rows(const T **p, long long *ld, int rows, int K, char **ws, hipStream_t st) {
-  const int per_row = (int)align_up(K, kCopyUnit) / 8;
-  const long long chunks = (long long)rows * per_row;
-  T *out = reinterpret_cast<T *>(*ws);
-  hipLaunchKernelGGL(align_rows_kernel<T>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, *p, *ld, chunks, per_row, K, out);
-  QUAMBA_LAUNCH_CHECK();
-  *p = out;
-  *ld = per_row * 8LL;
-  *ws += aligned_bytes(rows, K);
-  return QUAMBA_OK;
-}
-
 template <typename T, typename O>
 int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, void *ws, size_t ws_bytes,
                hipStream_t st) {
@@ -652,9 +649,13 @@ int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int 
   if (copies(M) && !(wx && ww) && ws && (wx ? 0 : aligned_bytes(M, K)) + (ww ? 0 : aligned_bytes(N, K)) <= ws_bytes &&
       g_linear_variant.load(std::memory_order_relaxed) < 0) {
     char *at = static_cast<char *>(ws);
-    int rc = wx ? QUAMBA_OK : align_rows(&x, &ldx, M, K, &at, st);
-    if (rc == QUAMBA_OK && !ww) rc = align_rows(&W, &ldw, N, K, &at, st);
-    if (rc != QUAMBA_OK) return rc;
+    const int per_row = (int)align_up(K, kCopyUnit) / 8;
+    const RowCopy<T> cx{x, ldx, wx ? 0 : (long long)M * per_row, reinterpret_cast<T *>(at)};
+    const RowCopy<T> cw{W, ldw, ww ? 0 : (long long)N * per_row, reinterpret_cast<T *>(at + (wx ? 0 : aligned_bytes(M, K)))};
+    hipLaunchKernelGGL(align_rows_kernel<T>, dim3((unsigned)((cx.chunks + cw.chunks + 255) / 256)), dim3(256), 0, st, cx, cw, per_row, K);
+    QUAMBA_LAUNCH_CHECK();
+    if (!wx) x = cx.to, ldx = per_row * 8LL;
+    if (!ww) W = cw.to, ldw = per_row * 8LL;
     wx = ww = true;
     K = (int)align_up(K, 8);  // no further: the other operand may not be a copy, and what stands behind its K is not zero
   }
