@@ -684,6 +684,9 @@ int quamba_probe_rate(int probe, int waves_per_simd, int iters, double *instr_pe
  * Host-only queries of what is chosen for a shape with the full workspace, for tests of the rules:
  *   quamba_debug_gemm_kind(M, N, K)    configuration of an int8 GEMM as quamba_debug_set_gemm_variant counts
  *                                      them, before the launcher cuts rows; -1 = few-row streaming kernel, -2 = not served
+ *   quamba_debug_linear_kind(M, N, K, ldx, ldw, ws_bytes)  configuration of quamba_linear for buffers that start on 16 bytes, as
+ *                                      quamba_debug_set_linear_variant counts them, + 16 where x is copied first and + 32 where
+ *                                      W is; -2 = not served
  *   quamba_debug_xfmt_column_tiles(M, N, K)  x_proj of the 8-bit float formats: column tiles per wave, 1 = the
  *                                      column groups are spread over the grid; 0 = not served
  *   quamba_debug_decode_stack_words(d_model, d_inner, dt_rank, batch, role, item, out, cap)  generation of a stack
@@ -710,6 +713,7 @@ void quamba_debug_set_decode_stack(int v);
 void quamba_debug_set_linear_variant(int v);
 void quamba_debug_set_linattn_blocks(int v);
 int quamba_debug_gemm_kind(int M, int N, int K);
+int quamba_debug_linear_kind(int M, int N, int K, int ldx, int ldw, size_t ws_bytes);
 int quamba_debug_xfmt_column_tiles(int M, int N, int K);
 int quamba_debug_decode_stack_words(int d_model, int d_inner, int dt_rank, int batch, int role, int item, int32_t *out, int cap);
 int quamba_debug_decode_stack_served(const quamba_dims *dims, int n_layers, int batch);

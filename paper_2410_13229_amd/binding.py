@@ -32,7 +32,7 @@ __all__ = [
     "quamba_debug_set_gemm_variant", "quamba_debug_set_gemm_split", "quamba_debug_set_gemv_max_rows",
     "quamba_debug_set_fuse_dt", "quamba_debug_set_fuse_decode", "quamba_debug_set_scan_variant",
     "quamba_debug_set_decode_stack", "quamba_debug_set_linear_variant", "quamba_debug_set_linattn_blocks",
-    "quamba_debug_gemm_kind", "quamba_debug_xfmt_column_tiles", "quamba_debug_last_block_reads_ahead",
+    "quamba_debug_gemm_kind", "quamba_debug_linear_kind", "quamba_debug_xfmt_column_tiles", "quamba_debug_last_block_reads_ahead",
     "quamba_debug_decode_stack_words", "quamba_debug_decode_stack_served",
     "quamba_debug_decode_reads_ahead", "quamba_debug_percentile_workgroups",
     "PROBE_FMA_F32", "PROBE_EXP_F32", "PROBE_SCAN_MIX", "PROBE_MFMA_I8", "PROBE_MFMA_I8_RANDOM",
@@ -372,6 +372,8 @@ def lib():
     for name in ("quamba_debug_gemm_kind", "quamba_debug_xfmt_column_tiles"):
         getattr(L, name).argtypes = [i, i, i]
         getattr(L, name).restype = i
+    L.quamba_debug_linear_kind.argtypes = [i, i, i, i, i, sz]
+    L.quamba_debug_linear_kind.restype = i
     L.quamba_debug_last_block_reads_ahead.argtypes = [i, i, i, i]
     L.quamba_debug_last_block_reads_ahead.restype = i
     L.quamba_debug_decode_stack_words.argtypes = [i, i, i, i, i, i, P(C.c_int32), i]
@@ -779,6 +781,10 @@ def quamba_debug_set_linattn_blocks(v):
 
 def quamba_debug_gemm_kind(M, N, K) -> int:
     return int(lib().quamba_debug_gemm_kind(int(M), int(N), int(K)))
+
+
+def quamba_debug_linear_kind(M, N, K, ldx, ldw, ws_bytes) -> int:
+    return int(lib().quamba_debug_linear_kind(int(M), int(N), int(K), int(ldx), int(ldw), int(ws_bytes)))
 
 
 def quamba_debug_xfmt_column_tiles(M, N, K) -> int:

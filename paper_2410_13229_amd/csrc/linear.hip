@@ -570,7 +570,7 @@ std::atomic<int> g_linear_variant{-1};
 //   6 = 64 x 64 (ring of 3)   7 = 32 x 32, 4 K groups   8 = 64 x 64, 2 K groups   9 = 128 x 128, 2 K groups   11 = 32 x 32, 8 K groups
 constexpr int kLinearKinds = 12;
 
-int plan_linear(int M, int N, int K, bool wide) {
+int pick_kind(int M, int N, int K, bool wide) {
   const int forced = g_linear_variant.load(std::memory_order_relaxed);
   if (forced >= 0 && forced < kLinearKinds && (forced != 2 || M <= 16) && (forced != 10 || M <= 4) && (forced < 3 || forced == 10 || wide))
     return forced;
@@ -630,14 +630,25 @@ int run_vec(const T *x, long long ldx, const T *W, long long ldw, int M, int N, 
   return QUAMBA_OK;
 }
 
-template <typename T>
-bool rows_wide(const T *p, long long ld, int K) {
-  return aligned(p, 16) && ld % 8 == 0 && K % 8 == 0 && ld < (1 << 21);  // a tile's rows lie within 2^31 bytes
-}
+// Rows that the direct-to-LDS kernels take: they start on 16 bytes, and a tile's (at most 320) lie within the 2^31 bytes that a lane's
+// offset reaches.
+constexpr int kLongRow = 1 << 21;
+bool rows_wide(const void *p, long long ld, int K) { return aligned(p, 16) && ld % 8 == 0 && K % 8 == 0 && ld < kLongRow; }
 constexpr int kCopyUnit = 64;  // elements a copied row is a multiple of: whole 128-byte lines
 size_t aligned_bytes(int rows, int K) { return align_up((size_t)rows * align_up(K, kCopyUnit) * 2, 256); }
-// More rows than the streaming kernels take: operands of any alignment are worth copying to 16-byte rows first
-bool copies(int M) { return M > 16; }
+// More rows than the streaming kernels take: operands of any alignment are worth copying to 16-byte rows first, unless the copies
+// would again be too long for the kernels that want them.
+bool copies(int M, int K) { return M > 16 && align_up(K, kCopyUnit) < kLongRow; }
+
+struct LinearPlan {
+  bool copy_x, copy_w;
+  int kind;
+};
+LinearPlan plan_linear(int M, int N, int K, bool wide_x, bool wide_w, size_t ws_bytes) {
+  const bool copy = copies(M, K) && !(wide_x && wide_w) && (wide_x ? 0 : aligned_bytes(M, K)) + (wide_w ? 0 : aligned_bytes(N, K)) <= ws_bytes &&
+                    g_linear_variant.load(std::memory_order_relaxed) < 0;
+  return LinearPlan{copy && !wide_x, copy && !wide_w, pick_kind(M, N, copy ? (int)align_up(K, 8) : K, copy || (wide_x && wide_w))};
+}
 
 template <typename T, typename O>
 int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, void *ws, size_t ws_bytes,
@@ -645,21 +656,19 @@ int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int 
   if (((M + 31LL) / 32) * ((N + 31LL) / 32) > INT_MAX)
     return fail(QUAMBA_EUNSUPPORTED, "linear: %d x %d outputs are more than one launch takes", M, N);
   if (M > 1 << 30 || N > 1 << 30 || K > 1 << 30) return fail(QUAMBA_EUNSUPPORTED, "linear: M=%d N=%d K=%d (at most 2^30 each)", M, N, K);
-  bool wx = rows_wide(x, ldx, K), ww = rows_wide(W, ldw, K);
-  if (copies(M) && !(wx && ww) && ws && (wx ? 0 : aligned_bytes(M, K)) + (ww ? 0 : aligned_bytes(N, K)) <= ws_bytes &&
-      g_linear_variant.load(std::memory_order_relaxed) < 0) {
+  const LinearPlan p = plan_linear(M, N, K, rows_wide(x, ldx, K), rows_wide(W, ldw, K), ws_bytes);
+  if (p.copy_x || p.copy_w) {
     char *at = static_cast<char *>(ws);
     const int per_row = (int)align_up(K, kCopyUnit) / 8;
-    const RowCopy<T> cx{x, ldx, wx ? 0 : (long long)M * per_row, reinterpret_cast<T *>(at)};
-    const RowCopy<T> cw{W, ldw, ww ? 0 : (long long)N * per_row, reinterpret_cast<T *>(at + (wx ? 0 : aligned_bytes(M, K)))};
+    const RowCopy<T> cx{x, ldx, p.copy_x ? (long long)M * per_row : 0, reinterpret_cast<T *>(at)};
+    const RowCopy<T> cw{W, ldw, p.copy_w ? (long long)N * per_row : 0, reinterpret_cast<T *>(at + (p.copy_x ? aligned_bytes(M, K) : 0))};
     hipLaunchKernelGGL(align_rows_kernel<T>, dim3((unsigned)((cx.chunks + cw.chunks + 255) / 256)), dim3(256), 0, st, cx, cw, per_row, K);
     QUAMBA_LAUNCH_CHECK();
-    if (!wx) x = cx.to, ldx = per_row * 8LL;
-    if (!ww) W = cw.to, ldw = per_row * 8LL;
-    wx = ww = true;
+    if (p.copy_x) x = cx.to, ldx = per_row * 8LL;
+    if (p.copy_w) W = cw.to, ldw = per_row * 8LL;
     K = (int)align_up(K, 8);  // no further: the other operand may not be a copy, and what stands behind its K is not zero
   }
-  switch (plan_linear(M, N, K, wx && ww)) {
+  switch (p.kind) {
     case 0: return run_any<T, O, 1, 1>(x, ldx, W, ldw, M, N, K, epi, st);
     case 1: return run_any<T, O, 2, 2>(x, ldx, W, ldw, M, N, K, epi, st);
     case 2:
@@ -694,7 +703,7 @@ size_t quamba_linear_workspace_bytes(int M, int N, int K) {
     fail(QUAMBA_EINVAL, "linear: M=%d N=%d K=%d", M, N, K);
     return 0;
   }
-  return copies(M) ? aligned_bytes(M, K) + aligned_bytes(N, K) : 256;
+  return copies(M, K) ? aligned_bytes(M, K) + aligned_bytes(N, K) : 256;
 }
 
 int quamba_linear(int type, const void *x, int ldx, const void *W, int ldw, const float *bias, const void *residual, int ldr,
@@ -728,3 +737,9 @@ int quamba_linear(int type, const void *x, int ldx, const void *W, int ldw, cons
 }  // extern "C"
 
 extern "C" void quamba_debug_set_linear_variant(int v) { quamba::g_linear_variant.store(v); }
+
+extern "C" int quamba_debug_linear_kind(int M, int N, int K, int ldx, int ldw, size_t ws_bytes) {
+  if (M <= 0 || N <= 0 || K <= 0 || ldx < K || ldw < K) return -2;
+  const quamba::LinearPlan p = quamba::plan_linear(M, N, K, quamba::rows_wide(nullptr, ldx, K), quamba::rows_wide(nullptr, ldw, K), ws_bytes);
+  return p.kind + (p.copy_x ? 16 : 0) + (p.copy_w ? 32 : 0);
+}
