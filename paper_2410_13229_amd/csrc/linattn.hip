@@ -116,8 +116,11 @@ int run_step(const LinAttnArgs &a, hipStream_t st) {
 //   pieces (24 bits) or two fp16 ones (22).  bf16 pieces have fp32's range.  fp16 operands (k, q) need fp16 partners, so a
 //   column of S or of the weighted v is first brought to the top of fp16's range by a power of two; v itself splits into two
 //   bf16 pieces exactly.
-// A decay of -infinity (or below fp32's range) is a reset: it adds nothing to G but starts a new stretch, and weights between
-// different stretches are 0.
+// A decay of -infinity (or below fp32's range) is a reset: it adds nothing to G, but weights across it are 0.
+//
+// The exponents G_t - G_s are differences of sums that grow by up to 126 a token, and what fp32 rounds off a sum of 2000 is 2^-14 of
+// a weight.  So a sum is held as a multiple of 2^-10 and a factor for the rest: with 200 for a reset (exp2 of -200 is 0) the
+// multiples stay below 64 * 200, 24 bits, and their differences are exact.
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kBlock = 64;
 
@@ -128,11 +131,11 @@ struct SegArgs {
 };
 
 struct GTable {  // of a block's 64 tokens
-  float d[kBlock];     // log2 decays summed from the token's group of 16 on
-  int n[kBlock];       // stretch (resets up to the token)
+  float d[kBlock];     // G_t to the nearest multiple of 2^-10, less 200 for each reset up to the token
+  float up[kBlock];    // scale exp2 of what the rounding left over,
+  float down[kBlock];  // and exp2 of its opposite: scale exp2(G_t - G_s) = exp2(d_t - d_s) up_t down_s
   float e[kBlock];     // scale exp2(G_t), 0 behind a reset
   float w[kBlock];     // exp2(G_64 - G_s), 0 in front of a reset
-  float between[16];   // 4 tb + sb: sums in front of group tb less those in front of group sb
   double sum;          // G_64
   double carry;        // what the factors applied so far are off by (their exact product over the applied one)
   float dec;           // the factor of the state
@@ -155,6 +158,9 @@ __device__ __forceinline__ double exp2_neg(double x) {
   p = __builtin_fma(p, f, 1.0);
   return __builtin_ldexp(p, (int)n);
 }
+
+// x to the nearest multiple of 2^-10
+__device__ __forceinline__ double coarse(double x) { return __builtin_rint(x * 1024.0) * (1.0 / 1024.0); }
 
 // A double moved by a DPP pattern, 0 where no lane supplies it.
 template <int CTRL>
@@ -185,15 +191,15 @@ __device__ __forceinline__ void make_table(float g, float scale, double carry, i
   const double G = d + (lane < 16 ? 0.0 : (lane < 32 ? b1 : (lane < 48 ? b2 : b3)));
   const unsigned long long m = __ballot(reset);
   const int n = __popcll(m & (~0ull >> (63 - lane))), last = __popcll(m);
-  t.d[lane] = (float)d;
-  t.n[lane] = n;
-  t.e[lane] = n ? 0.f : scale * __builtin_amdgcn_exp2f((float)G);
-  t.w[lane] = n != last ? 0.f : __builtin_amdgcn_exp2f((float)(all - G));
+  const double Gc = coarse(G), W = all - G, Wc = coarse(W);
+  const float up = scale * __builtin_amdgcn_exp2f((float)(G - Gc));
+  t.d[lane] = (float)(Gc - 200.0 * n);
+  t.up[lane] = up;
+  t.down[lane] = __builtin_amdgcn_exp2f((float)(Gc - G));
+  t.e[lane] = n ? 0.f : __builtin_amdgcn_exp2f((float)Gc) * up;
+  t.w[lane] = n != last ? 0.f : __builtin_amdgcn_exp2f((float)Wc) * __builtin_amdgcn_exp2f((float)(W - Wc));
   const double dec = last ? 0.0 : exp2_neg(all) * carry;
   const float used = (float)dec;
-  const int tb = lane >> 2, sb = lane & 3;
-  const double bt = tb == 0 ? 0.0 : (tb == 1 ? b1 : (tb == 2 ? b2 : b3)), bs = sb == 0 ? 0.0 : (sb == 1 ? b1 : (sb == 2 ? b2 : b3));
-  if (lane < 16) t.between[lane] = (float)(bt - bs);
   if (lane == 0) {
     t.sum = all;
     t.carry = used > 1e-30f ? dec / (double)used : 1.0;
@@ -550,18 +556,14 @@ __global__ __launch_bounds__(256, KT == 8 && OUT ? 1 : 2) void linattn_blocks_ke
             p[x] = Half<T>::mfma16(*reinterpret_cast<const v8 *>(lks + buf * TB + 16 * (sb + x) * 64 * KT + at), fq, p[x]);  // rows s, columns t
         }
         const int t = 16 * tb + c;
-        const float d_t = tab.d[t];
-        const int n_t = tab.n[t];
+        const float d_t = tab.d[t], up = tab.up[t];
 #pragma unroll
         for (int x = 0; x < B; ++x) {
           const int s = 16 * (sb + x) + 4 * g;
-          const float dt = d_t + tab.between[4 * tb + sb + x];
-          const v4f ds = *reinterpret_cast<const v4f *>(&tab.d[s]);
-          const int4 ns = *reinterpret_cast<const int4 *>(&tab.n[s]);
-          const int nn[4] = {ns.x, ns.y, ns.z, ns.w};
+          const v4f ds = *reinterpret_cast<const v4f *>(&tab.d[s]), down = *reinterpret_cast<const v4f *>(&tab.down[s]);
           float v[4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] = s + r <= t && nn[r] == n_t ? a.scale * p[x][r] * __builtin_amdgcn_exp2f(dt - ds[r]) : 0.f;
+          for (int r = 0; r < 4; ++r) v[r] = s + r <= t ? up * p[x][r] * (down[r] * __builtin_amdgcn_exp2f(d_t - ds[r])) : 0.f;
           const int at = weight_at(t, 2 * (sb + x) + (g >> 1)) + (g & 1) * 8;
           uint2 w;
           w.x = take2(v[0], v[1], __bf16());

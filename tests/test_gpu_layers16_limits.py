@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2410_13229_amd as Q
+from test_gpu_linattn import Call, U, _f64
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -22,3 +23,53 @@ def test_linear_rows_of_more_than_two_million_elements_with_a_workspace():
         out = torch.full((M, N), float("nan"), device=DEV)
         Q.quamba_linear(Q.TYPE_F16, x, K, W, K, None, None, 0, M, N, K, Q.ACT_NONE, Q.TYPE_F32, out, N, room)
         assert np.array_equal(out.cpu().numpy(), a.cpu().numpy().astype(np.float32) @ b.cpu().numpy().astype(np.float32).T)
+
+
+def _closely(c, want):
+    """Call.check's bounds without a term for the decays: their sums keep 33 bits or more in front of the binary point's 2^-10, so a weight
+    is off by its exponential's unit and two roundings, which the 16 units of 2^-23 hold."""
+    out, S, out_size, size = want
+    e = torch.finfo(c.dt)
+    t_out = ((c.L + c.dk + 64 + 16) * U + 2.0 ** -16) * out_size
+    t_out = t_out + e.eps / 2 * (np.abs(out) + t_out) + e.smallest_normal * e.eps
+    got = _f64(c.out[..., :c.Hv * c.dv]).reshape(out.shape)
+    off = np.abs(got - out) / t_out
+    assert off.max() <= 1, "output off by %.2f of what it may be" % off.max()
+    off = np.abs(_f64(c.state) - S) / (((c.L + 16 + 64) * U + 2.0 ** -21) * size + 1e-37)
+    assert off.max() <= 1, "state off by %.2f of what it may be" % off.max()
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 64, 1, 64, 8, 16), (1, 64, 1, 64, 7, 5), (2, 64, 1, 16, 128, 128), (2, 64, 1, 8, 256, 64)])
+def test_linattn_weights_behind_steep_decays(shape, dt):
+    """One block: 13 tokens that forget nearly everything, then 3 that forget little, whose contributions cancel.  What the sums of the
+    log decays have reached by then (about 1600 in a group of 16 tokens) must not show in the weights between the 3.  q, k and v are
+    whole numbers that every piece holds, so a weight is off by its two bf16 pieces (each leaves 2^-9 of what it takes: 2^-18), and
+    dk + 64 + 16 fp32 operations, then the rounding to the output."""
+    B, L, _, Hv, dk, dv = shape
+    g = torch.Generator(device=DEV).manual_seed(L)
+    for first in (13, 15):  # the 3 at the end of a group of 16 tokens, or across its border
+        c = Call(*shape, dt, decay="none", state=False)
+        q, k, v = c.parts()
+        q.fill_(1.0), k.fill_(1.0)
+        v.copy_((torch.arange(L, device=DEV) % 2 * 2.0 - 1.0)[None, :, None].expand_as(v))
+        steep = -80 - 7 * torch.rand((B, L, Hv), generator=g, device=DEV)
+        weak = -0.02 * torch.rand((B, L, Hv), generator=g, device=DEV)
+        c.g = torch.where(((torch.arange(L, device=DEV) - first) % 16 < 3)[None, :, None], weak, steep)
+        out, _, size, _ = c.want()
+        c.prefill()
+        tol = ((dk + 64 + 16) * U / 2 + 2.0 ** -18) * size
+        e = torch.finfo(dt)
+        tol = tol + e.eps / 2 * (np.abs(out) + tol) + e.smallest_normal * e.eps
+        off = np.abs(_f64(c.out[..., :Hv * dv]).reshape(out.shape) - out) / tol
+        assert off.max() <= 1, "output off by %.2f of what it may be" % off.max()
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("decay", ["token", "strong", "reset"])
+@pytest.mark.parametrize("shape", [(2, 150, 1, 2, 64, 64), (1, 700, 2, 4, 128, 64), (1, 300, 1, 1, 40, 130)])
+def test_linattn_decays_closely(shape, decay, dt):
+    c = Call(*shape, dt, decay=decay)
+    want = c.want()
+    c.prefill()
+    _closely(c, want)
