@@ -73,3 +73,30 @@ def test_linattn_decays_closely(shape, decay, dt):
     want = c.want()
     c.prefill()
     _closely(c, want)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("shape, token, reset", [((1, 64, 1, 2, 64, 64), 20, 24), ((1, 200, 2, 2, 33, 19), 70, 100), ((2, 130, 1, 2, 128, 128), 3, 63),
+                                                 ((1, 130, 1, 1, 256, 40), 60, 70)])
+def test_linattn_a_reset_does_not_clear_a_bad_token(shape, token, reset, dt):
+    """NaN in k or in the decay reaches its head from its token on, also behind a reset in the same block; one in v its column."""
+    B, L, Hk, Hv, dk, dv = shape
+    for where in ("k", "decay", "v"):
+        c = Call(*shape, dt)
+        c.g[:, reset] = -float("inf")
+        q, k, v = c.parts()
+        if where == "k":
+            k[0, token, 0] = float("nan")
+        elif where == "decay":
+            c.g[0, token, 0] = float("nan")
+        else:
+            v[0, token, dv // 2] = float("inf")
+        c.prefill()
+        out = c.out.view(B, L, Hv, dv)
+        hit = torch.zeros((B, L, Hv, dv), dtype=torch.bool, device=DEV)
+        if where == "v":
+            hit[0, token:, 0, dv // 2] = True
+        else:
+            hit[0, token:, :Hv // Hk if where == "k" else 1] = True
+        bad = ~torch.isfinite(out)
+        assert int((bad != hit).sum()) == 0, where
