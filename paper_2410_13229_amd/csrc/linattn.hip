@@ -28,8 +28,11 @@ struct LinAttnArgs {
 
 constexpr float LOG2E = 1.44269504088896340736f;
 
+// Below ln 2^-126 exp leaves fp32's normal range: nothing of the past remains.
+__device__ __forceinline__ bool forgets(float g) { return g < -87.33654f; }
+
 // a = exp(min(g, 0)); NaN stays NaN, -inf gives 0
-__device__ __forceinline__ float decay_of(float g) { return __builtin_amdgcn_exp2f((g > 0.f ? 0.f : g) * LOG2E); }
+__device__ __forceinline__ float decay_of(float g) { return forgets(g) ? 0.f : __builtin_amdgcn_exp2f((g > 0.f ? 0.f : g) * LOG2E); }
 
 // One token: bound by reading and writing the state (64 sequences, 80 heads of 128 x 64: 336 MB, at the rate a copy reaches 66 us).
 // A workgroup takes 64 columns of one head's state, rows in turn over its threads, V columns a thread (4: 16-byte accesses along
@@ -180,7 +183,7 @@ __device__ __forceinline__ double lane_f64(double v, int lane) {
 // fp32 factor per block, and the roundings of a hundred equal factors would add up; so each is rounded from the exact one times
 // what the product so far is off by, which keeps the product over any run of blocks within two roundings.
 __device__ __forceinline__ void make_table(float g, float scale, double carry, int lane, GTable &t) {
-  const bool reset = g < -87.f;  // exp leaves fp32's normal range: nothing of the past remains
+  const bool reset = forgets(g);
   const double x = reset || g > 0.f ? 0.0 : (double)g * 1.44269504088896340736;
   double d = x;  // inclusive sums inside rows of 16 lanes
   d += dpp_f64<0x111>(d);  // row_shr 1

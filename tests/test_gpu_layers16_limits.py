@@ -100,3 +100,29 @@ def test_linattn_a_reset_does_not_clear_a_bad_token(shape, token, reset, dt):
             hit[0, token:, :Hv // Hk if where == "k" else 1] = True
         bad = ~torch.isfinite(out)
         assert int((bad != hit).sum()) == 0, where
+
+
+@pytest.mark.parametrize("form", ["prefill", "step"])
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+def test_linattn_forgets_where_the_decay_leaves_the_normal_range(dt, form):
+    """exp(g) >= 2^-126 decays, below that nothing of the past remains; both forms draw the line at the same g."""
+    B, Hk, Hv, dk, dv = 1, 1, 6, 64, 64
+    c = Call(B, 1, Hk, Hv, dk, dv, dt)
+    q, k, v = c.parts()
+    q.fill_(1.0), k.zero_(), v.zero_()
+    c.g = torch.tensor([-86.9, -87.2, -87.33654, -87.33656, -87.5, -100.0], device=DEV).view(1, 1, Hv)
+    c.state = torch.full((B, Hv, dk, dv), 2.0 ** 100, device=DEV)
+    a = np.exp(_f64(c.g).ravel())
+    a[3:] = 0.0
+    if form == "prefill":
+        c.prefill()
+    else:
+        c.step(0, c.state, c.out[:, 0])
+    want = a[:, None, None] * 2.0 ** 100 * np.ones((dk, dv))
+    got = _f64(c.state)[0]
+    assert (got[3:] == 0).all() and (_f64(c.out).reshape(Hv, dv)[3:] == 0).all()
+    # the exponent, 126 in the worst case, is rounded to fp32 once or twice: 2 * 126 / 2^24, times ln 2
+    assert (np.abs(got - want) <= 2 * 126 * 2.0 ** -24 * want).all()
+    if dt == torch.bfloat16:  # 64 of them, scaled: about 1e-7, far below fp16
+        out = c.scale * dk * want[:, 0]
+        assert (np.abs(_f64(c.out).reshape(Hv, dv) - out) <= (2.0 ** -8 + 2.0 ** -15) * out).all()
