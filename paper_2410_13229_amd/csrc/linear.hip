@@ -5,6 +5,7 @@
 // The operands go through the matrix units as they are (products of 16-bit values are exact in fp32), sums stay in
 // fp32 up to the epilogue, and the result is rounded once, to the output's type.
 #include <atomic>
+#include <cfloat>
 #include <climits>
 
 #include "common.h"
@@ -41,21 +42,27 @@ __device__ __forceinline__ float upper_tail(float z) {
   return p * t * __builtin_amdgcn_exp2f(-0.72134752044448170368f * z * z);
 }
 
-// The activation in fp32.  exp2 of a large argument is infinite and its reciprocal 0, so nothing overflows on the way; v * 0 at
-// v = -infinity would be NaN where the limit is 0.
+// v sigmoid(a) for a of v's sign.  The denominator is held 2^-8 times as large, so its reciprocal is not flushed before the result
+// leaves fp32's normal range (SILU(-88) = -5e-37); nothing overflows on the way.  -infinity counts as the lowest number, whose
+// product with 0 is the limit 0; a NaN comes back from the exponential.
+__device__ __forceinline__ float times_sigmoid(float v, float a) {
+  constexpr float LOG2E = 1.44269504088896340736f, D = 0.00390625f;
+  return fmaxf(v, -FLT_MAX) * (__builtin_amdgcn_rcpf(D + __builtin_amdgcn_exp2f(fmaf(-LOG2E, a, -8.f))) * D);
+}
+
+// The activation in fp32.  exp2 of a large argument is infinite and its reciprocal 0, so nothing overflows on the way.
 __device__ __forceinline__ float activate(float v, int act) {
   constexpr float LOG2E = 1.44269504088896340736f;
   switch (act) {
     case QUAMBA_ACT_RELU: return v < 0.f ? 0.f : v;  // keeps NaN
-    case QUAMBA_ACT_SILU: return v == -INFINITY ? 0.f : v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-v * LOG2E));
+    case QUAMBA_ACT_SILU: return times_sigmoid(v, v);
     case QUAMBA_ACT_GELU: {  // v Phi(v)
       const float u = upper_tail(fabsf(v)), phi = v < 0.f ? u : 1.f - u;
       return phi == 0.f ? 0.f : v * phi;
     }
     case QUAMBA_ACT_GELU_TANH: {  // 0.5 v (1 + tanh u) = v sigmoid(2 u), u = sqrt(2 / pi) (v + 0.044715 v^3)
       const float u2 = 1.59576912160573071176f * v * (1.f + 0.044715f * v * v);
-      const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-u2 * LOG2E));
-      return s == 0.f ? 0.f : v * s;
+      return times_sigmoid(v, u2);
     }
     case QUAMBA_ACT_SIGMOID: return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-v * LOG2E));
     default: return v;

@@ -1,4 +1,6 @@
 """The 16-bit layers near the limits of their sizes and values."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -126,3 +128,26 @@ def test_linattn_forgets_where_the_decay_leaves_the_normal_range(dt, form):
     if dt == torch.bfloat16:  # 64 of them, scaled: about 1e-7, far below fp16
         out = c.scale * dk * want[:, 0]
         assert (np.abs(_f64(c.out).reshape(Hv, dv) - out) <= (2.0 ** -8 + 2.0 ** -15) * out).all()
+
+
+@pytest.mark.parametrize("act, lowest", [("silu", -104.0), ("gelu", -14.5), ("gelu_tanh", -11.0), ("sigmoid", -88.0)])
+@pytest.mark.parametrize("M", [1, 70])
+def test_linear_tails_of_the_activations(act, lowest, M):
+    """Far negative arguments, whose results are small but normal numbers of fp32 and bf16.  What a result may be off by relative to itself: 16
+    units of 2^-23 for the operations, the exponent's rounding (|v|, of GELU v^2, of its tanh form four roundings of 2 u), half a step of the
+    output; numbers below the smallest normal one may be 0."""
+    N = 4096
+    v = torch.linspace(lowest, 8.0, N, device=DEV)
+    x, W = torch.zeros((M, 64), dtype=torch.bfloat16, device=DEV), torch.zeros((N, 64), dtype=torch.bfloat16, device=DEV)
+    b = v.double().cpu().numpy()
+    u2 = 2 * math.sqrt(2 / math.pi) * (b + 0.044715 * b ** 3)
+    want = {"silu": lambda: b / (1 + np.exp(-b)), "gelu": lambda: np.array([0.5 * t * math.erfc(-t / math.sqrt(2)) for t in b]),
+            "gelu_tanh": lambda: b / (1 + np.exp(-u2)), "sigmoid": lambda: 1 / (1 + np.exp(-b))}[act]()
+    exponent = {"silu": np.abs(b), "gelu": b * b, "gelu_tanh": 4 * np.abs(u2), "sigmoid": np.abs(b)}[act]
+    for out_type, dt in ((Q.TYPE_F32, torch.float32), (Q.TYPE_BF16, torch.bfloat16)):
+        out = torch.full((M, N), float("nan"), dtype=dt, device=DEV)
+        Q.quamba_linear(Q.TYPE_BF16, x, 64, W, 64, v, None, 0, M, N, 64, getattr(Q, "ACT_" + act.upper()), out_type, out, N, None)
+        off = np.abs(_f64(out) - want)
+        tol = (16 + exponent) * U * np.abs(want) + torch.finfo(dt).eps / 2 * np.abs(want) + 2.0 ** -126
+        worst = float((off / tol).max())
+        assert worst <= 1, "%.2f of what it may be, at %g" % (worst, b[int((off / tol).max(0).argmax())])
