@@ -609,7 +609,9 @@ int quamba_linear(int type, const void *x, int ldx, const void *W, int ldw, cons
  * quamba_linattn_prefill runs prompts: lens int32 [Bt] (device, may be NULL = L each) gives each sequence's length, clamped to
  * [0, L]; tokens behind it are not read, their output rows are left as they were, and an empty sequence keeps its state.  The sums are
  * taken block by block: the result is that of the recurrence up to the rounding of fp32 sums (block weights carry 16 bits or more,
- * the state's update 22 or more).  Workspace: quamba_linattn_workspace_bytes, 256-byte aligned.
+ * the state's update 22 or more).  ws (256-byte aligned, may be NULL): with quamba_linattn_workspace_bytes a sequence is cut into as
+ * many segments as pay; with less, into fewer (one needs no room), which may take twice the time and adds the sums in another order.  A
+ * larger batch or prompt may need less, so a program with several shapes takes the largest of their queries.
  * Infinities and NaN stay out of everything before their token: one in v makes its column of outputs and state NaN or infinite
  * from its token on, one in k or g its head's; a reset does not clear a state that holds one.
  * quamba_linattn_step is one token of every sequence (L = 1, state required), strides between sequences.
@@ -687,6 +689,8 @@ int quamba_probe_rate(int probe, int waves_per_simd, int iters, double *instr_pe
  *   quamba_debug_linear_kind(M, N, K, ldx, ldw, ws_bytes)  configuration of quamba_linear for buffers that start on 16 bytes, as
  *                                      quamba_debug_set_linear_variant counts them, + 16 where x is copied first and + 32 where
  *                                      W is; -2 = not served
+ *   quamba_debug_linattn_blocks(Bt, L, Hv, dk, dv, ws_bytes)  blocks of 64 tokens in a segment of quamba_linattn_prefill with a workspace
+ *                                      of ws_bytes; -2 = not served
  *   quamba_debug_xfmt_column_tiles(M, N, K)  x_proj of the 8-bit float formats: column tiles per wave, 1 = the
  *                                      column groups are spread over the grid; 0 = not served
  *   quamba_debug_decode_stack_words(d_model, d_inner, dt_rank, batch, role, item, out, cap)  generation of a stack
@@ -714,6 +718,7 @@ void quamba_debug_set_linear_variant(int v);
 void quamba_debug_set_linattn_blocks(int v);
 int quamba_debug_gemm_kind(int M, int N, int K);
 int quamba_debug_linear_kind(int M, int N, int K, int ldx, int ldw, size_t ws_bytes);
+int quamba_debug_linattn_blocks(int Bt, int L, int Hv, int dk, int dv, size_t ws_bytes);
 int quamba_debug_xfmt_column_tiles(int M, int N, int K);
 int quamba_debug_decode_stack_words(int d_model, int d_inner, int dt_rank, int batch, int role, int item, int32_t *out, int cap);
 int quamba_debug_decode_stack_served(const quamba_dims *dims, int n_layers, int batch);

@@ -32,7 +32,7 @@ __all__ = [
     "quamba_debug_set_gemm_variant", "quamba_debug_set_gemm_split", "quamba_debug_set_gemv_max_rows",
     "quamba_debug_set_fuse_dt", "quamba_debug_set_fuse_decode", "quamba_debug_set_scan_variant",
     "quamba_debug_set_decode_stack", "quamba_debug_set_linear_variant", "quamba_debug_set_linattn_blocks",
-    "quamba_debug_gemm_kind", "quamba_debug_linear_kind", "quamba_debug_xfmt_column_tiles", "quamba_debug_last_block_reads_ahead",
+    "quamba_debug_gemm_kind", "quamba_debug_linear_kind", "quamba_debug_linattn_blocks", "quamba_debug_xfmt_column_tiles", "quamba_debug_last_block_reads_ahead",
     "quamba_debug_decode_stack_words", "quamba_debug_decode_stack_served",
     "quamba_debug_decode_reads_ahead", "quamba_debug_percentile_workgroups",
     "PROBE_FMA_F32", "PROBE_EXP_F32", "PROBE_SCAN_MIX", "PROBE_MFMA_I8", "PROBE_MFMA_I8_RANDOM",
@@ -374,6 +374,8 @@ def lib():
         getattr(L, name).restype = i
     L.quamba_debug_linear_kind.argtypes = [i, i, i, i, i, sz]
     L.quamba_debug_linear_kind.restype = i
+    L.quamba_debug_linattn_blocks.argtypes = [i, i, i, i, i, sz]
+    L.quamba_debug_linattn_blocks.restype = i
     L.quamba_debug_last_block_reads_ahead.argtypes = [i, i, i, i]
     L.quamba_debug_last_block_reads_ahead.restype = i
     L.quamba_debug_decode_stack_words.argtypes = [i, i, i, i, i, i, P(C.c_int32), i]
@@ -730,7 +732,7 @@ def quamba_linattn_workspace_bytes(Bt, L, Hk, Hv, dk, dv) -> int:
 
 def quamba_linattn_prefill(type, q, ldq, k, ldk, v, ldv, log_decay, ldg, lens, Bt, L, Hk, Hv, dk, dv, scale, out, ldo, state, ws,
                            stream=None):
-    """Prompts; `log_decay`, `lens` and `state` may be None."""
+    """Prompts; `log_decay`, `lens`, `state` and `ws` may be None."""
     _check(lib().quamba_linattn_prefill(type, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(log_decay), ldg, _ptr(lens), Bt, L, Hk,
                                         Hv, dk, dv, float(scale), _ptr(out), ldo, _ptr(state), _ptr(ws), _nbytes(ws),
                                         _stream(stream)))
@@ -785,6 +787,10 @@ def quamba_debug_gemm_kind(M, N, K) -> int:
 
 def quamba_debug_linear_kind(M, N, K, ldx, ldw, ws_bytes) -> int:
     return int(lib().quamba_debug_linear_kind(int(M), int(N), int(K), int(ldx), int(ldw), int(ws_bytes)))
+
+
+def quamba_debug_linattn_blocks(Bt, L, Hv, dk, dv, ws_bytes) -> int:
+    return int(lib().quamba_debug_linattn_blocks(int(Bt), int(L), int(Hv), int(dk), int(dv), int(ws_bytes)))
 
 
 def quamba_debug_xfmt_column_tiles(M, N, K) -> int:

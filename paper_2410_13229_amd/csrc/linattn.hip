@@ -925,13 +925,21 @@ struct AttnPlan {
   int kt, nt, segments, blocks;
 };
 
+size_t slots_bytes(const AttnPlan &p, int Bt, int Hv, int dk, int dv) {
+  return align_up((size_t)Bt * Hv * p.segments * dk * dv * sizeof(float), 256);
+}
+size_t prefill_workspace(const AttnPlan &p, int Bt, int Hv, int dk, int dv) {
+  return p.segments > 1 ? slots_bytes(p, Bt, Hv, dk, dv) + align_up((size_t)Bt * Hv * p.segments * sizeof(float2), 256) : 256;
+}
+
 // How many segments a sequence is cut into: the cheapest by a cost in us fitted to measured times.  One segment is one launch of
 // about 5 and 0.72 c a block; more are three launches, 9, whose two passes together take c a block and 3 to start, 1.42 times that
 // with two workgroups on a CU, plus the sums' way through memory and the chain that joins them.  At 32 shapes (1 to 80 heads, 128
 // to 65536 tokens, dk 32 to 256) the choice is within 10 % of the best of up to 16 that were timed: 1 x 2048, 80 heads of 128 x 64,
 // 6 blocks a segment 58 us, 4 66, 8 67, all in one 115; 8 x 256, 16 heads of 64 x 64, all in one 15.5, 2 blocks 21.5, single ones
 // 23.7; 1 x 16384, one head of 64 x 64, 3 blocks 33, single ones 44, all in one 617.
-AttnPlan plan_prefill(int Bt, int L, int Hv, int dk, int dv) {
+// What `room` does not hold is left out; one segment needs none, so a workspace that another shape asked for serves too.
+AttnPlan plan_prefill(int Bt, int L, int Hv, int dk, int dv, size_t room = SIZE_MAX) {
   AttnPlan p{2, 1, 1, 1};
   if (Bt == 0 || L == 0) return p;
   p.kt = dk <= 64 ? 2 : (dk <= 128 ? 4 : 8);
@@ -949,6 +957,8 @@ AttnPlan plan_prefill(int Bt, int L, int Hv, int dk, int dv) {
   if (pairs <= 65535)
     for (long long b = 1; b < blocks; b = b < 4 ? b + 1 : b + b / 4) {
       const double n = (double)((blocks + b - 1) / b);
+      p.segments = (int)n;
+      if (prefill_workspace(p, Bt, Hv, dk, dv) > room) continue;
       const double t = 9 + rounds(pairs * parts * n) * (c * b + 3) + pairs * n * dk * dv * 8.0 / 4e6 + 0.12 * n;
       if (t < best) best = t, at = b;
     }
@@ -957,13 +967,6 @@ AttnPlan plan_prefill(int Bt, int L, int Hv, int dk, int dv) {
   p.blocks = (int)at;
   p.segments = (int)((blocks + at - 1) / at);
   return p;
-}
-
-size_t slots_bytes(const AttnPlan &p, int Bt, int Hv, int dk, int dv) {
-  return align_up((size_t)Bt * Hv * p.segments * dk * dv * sizeof(float), 256);
-}
-size_t prefill_workspace(const AttnPlan &p, int Bt, int Hv, int dk, int dv) {
-  return p.segments > 1 ? slots_bytes(p, Bt, Hv, dk, dv) + align_up((size_t)Bt * Hv * p.segments * sizeof(float2), 256) : 256;
 }
 
 template <typename T, int KT, int NT, bool WIDE>
@@ -1048,7 +1051,7 @@ int quamba_linattn_prefill(int type, const void *q, int ldq, const void *k, int 
   const int rc = check("linattn_prefill", type, a);
   if (rc != QUAMBA_OK || Bt == 0 || L == 0) return rc;
   if (ws && !aligned(ws, 256)) return fail(QUAMBA_EINVAL, "linattn_prefill: workspace must be 256-byte aligned");
-  const AttnPlan p = plan_prefill(Bt, L, Hv, dk, dv);
+  const AttnPlan p = plan_prefill(Bt, L, Hv, dk, dv, ws ? ws_bytes : 0);
   if (p.segments > 1 && (!ws || ws_bytes < prefill_workspace(p, Bt, Hv, dk, dv)))
     return fail(QUAMBA_EWORKSPACE, "linattn_prefill: workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, prefill_workspace(p, Bt, Hv, dk, dv));
   hipStream_t st = as_stream(stream);
@@ -1070,3 +1073,8 @@ int quamba_linattn_step(int type, const void *q, int ldq, const void *k, int ldk
 }  // extern "C"
 
 extern "C" void quamba_debug_set_linattn_blocks(int v) { quamba::g_segment_blocks.store(v); }
+
+extern "C" int quamba_debug_linattn_blocks(int Bt, int L, int Hv, int dk, int dv, size_t ws_bytes) {
+  if (Bt <= 0 || L <= 0 || Hv <= 0 || dk <= 0 || dv <= 0 || dk > 256 || dv > 1024) return -2;
+  return quamba::plan_prefill(Bt, L, Hv, dk, dv, ws_bytes).blocks;
+}

@@ -151,3 +151,18 @@ def test_linear_tails_of_the_activations(act, lowest, M):
         tol = (16 + exponent) * U * np.abs(want) + torch.finfo(dt).eps / 2 * np.abs(want) + 2.0 ** -126
         worst = float((off / tol).max())
         assert worst <= 1, "%.2f of what it may be, at %g" % (worst, b[int((off / tol).max(0).argmax())])
+
+
+@pytest.mark.parametrize("shape", [(1, 700, 1, 2, 128, 64), (3, 333, 1, 1, 33, 19)])
+def test_linattn_with_any_workspace(shape):
+    """What the query of another shape gave, or nothing: right all the same."""
+    need = Q.quamba_linattn_workspace_bytes(*shape)
+    assert need > 256
+    for room in (None, 256, need // 2, need, 2 * need):
+        c = Call(*shape, torch.bfloat16)
+        want = c.want()
+        q, k, v = c.parts()
+        ws = None if room is None else torch.full((room,), 255, dtype=torch.uint8, device=DEV)
+        ld = c.rows.stride(1)
+        Q.quamba_linattn_prefill(Q.TYPE_BF16, q, ld, k, ld, v, ld, c.g, c.Hv, None, *shape, c.scale, c.out, c.out.stride(1), c.state, ws)
+        c.check(want)

@@ -29,3 +29,19 @@ def test_only_what_needs_a_copy_is_copied():
     assert COPY_X <= Q.quamba_debug_linear_kind(64, 96, 136, 137, 136, _room(64, 96, 136)) < COPY_W
     assert Q.quamba_debug_linear_kind(64, 96, LONG, 1 << 22, LONG, 1 << 40) == 0  # x and W alike
     assert Q.quamba_debug_linear_kind(16, 96, 135, 135, 135, 1 << 20) == 2  # few rows stream
+
+
+def test_linattn_cuts_a_prompt_into_as_many_segments_as_the_workspace_holds():
+    """80 heads of 128 x 64: four prompts of 2048 tokens ask for nothing, one of them for room for its segments."""
+    small, large = (Q.quamba_linattn_workspace_bytes(b, 2048, 1, 80, 128, 64) for b in (4, 1))
+    assert small == 256 and large > 1 << 20
+    assert Q.quamba_debug_linattn_blocks(4, 2048, 80, 128, 64, small) == 32
+    assert Q.quamba_debug_linattn_blocks(1, 2048, 80, 128, 64, large) < 32
+    last = 0
+    for room in (0, 256, large // 3, large // 2, large - 1, large, 1 << 40):
+        blocks = Q.quamba_debug_linattn_blocks(1, 2048, 80, 128, 64, room)
+        segments = -(-32 // blocks)
+        assert segments >= last  # never fewer with more room
+        assert segments == 1 or segments * 80 * (128 * 64 * 4 + 8) <= room
+        last = segments
+    assert Q.quamba_debug_linattn_blocks(1, 2048, 80, 128, 64, 0) == 32
