@@ -21,6 +21,9 @@ inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
+// A launch counts its threads along a dimension in 32 bits.
+inline bool launchable(long long workgroups, int threads) { return workgroups * threads <= 0xffffffffLL; }
+
 // (k, m) with n = k * 2^m, k in {1, 12, 20}; false if there is none.
 bool hadamard_factor(int n, int *k, int *m);
 

@@ -958,7 +958,7 @@ AttnPlan plan_prefill(int Bt, int L, int Hv, int dk, int dv, size_t room = SIZE_
     for (long long b = 1; b < blocks; b = b < 4 ? b + 1 : b + b / 4) {
       const double n = (double)((blocks + b - 1) / b);
       p.segments = (int)n;
-      if (prefill_workspace(p, Bt, Hv, dk, dv) > room) continue;
+      if (prefill_workspace(p, Bt, Hv, dk, dv) > room || !launchable((long long)(pairs * parts * n), 256)) continue;
       const double t = 9 + rounds(pairs * parts * n) * (c * b + 3) + pairs * n * dk * dv * 8.0 / 4e6 + 0.12 * n;
       if (t < best) best = t, at = b;
     }
@@ -973,7 +973,7 @@ template <typename T, int KT, int NT, bool WIDE>
 int run_blocks(const LinAttnArgs &a, const AttnPlan &p, void *ws, hipStream_t st) {
   const int parts = (a.dv + 64 * NT - 1) / (64 * NT);
   const long long one = (long long)parts * a.Bt * a.Hv;
-  if (one * p.segments > INT_MAX)
+  if (!launchable(one * p.segments, 256))
     return fail(QUAMBA_EUNSUPPORTED, "linattn_prefill: %d sequences of %d heads are more than one launch takes", a.Bt, a.Hv);
   SegArgs sg{p.segments, p.blocks, static_cast<float *>(ws), nullptr};
   if (p.segments > 1) {

@@ -550,7 +550,9 @@ __global__ __launch_bounds__(256) void linear_vec_kernel(const T *__restrict__ x
 }
 
 // Rows of any alignment copied to rows of a multiple of 64 elements, zeros behind K: both operands in one launch (or one of them:
-// the other has no chunks).  A division of 64 bits is as long as the copy, so only what needs one does it.
+// the other has no chunks).  A division of 64 bits is as long as the copy, so only what needs one does it.  A launch counts its threads
+// along a dimension in 32 bits, hence the second one.
+constexpr long long kCopyGrid = 1 << 20;
 template <typename T>
 struct RowCopy {
   const T *from;
@@ -559,7 +561,7 @@ struct RowCopy {
 };
 template <typename T>
 __global__ __launch_bounds__(256) void align_rows_kernel(RowCopy<T> a, RowCopy<T> b, int per_row, int K) {
-  long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  long long i = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
   const bool second = i >= a.chunks;
   if (second) i -= a.chunks;
   const RowCopy<T> &c = second ? b : a;
@@ -598,6 +600,8 @@ int pick_kind(int M, int N, int K, bool wide) {
   return e3 < e4 && e3 < e5 ? 3 : (e4 <= e5 ? 4 : 5);
 }
 
+int too_large(int M, int N) { return fail(QUAMBA_EUNSUPPORTED, "linear: %d x %d outputs are more than one launch takes", M, N); }
+
 template <typename T, typename O, int BM, int BN, int WGM, int WGN, int S, int BKB, int OCC, int KG>
 int run_dma(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, hipStream_t st) {
   constexpr int lds = S * (BM + BN) * BKB;
@@ -612,6 +616,7 @@ int run_dma(const T *x, long long ldx, const T *W, long long ldw, int M, int N, 
     attr_set.fetch_or(bit, std::memory_order_release);
   }
   const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
+  if (!launchable((long long)tiles_m * tiles_n, 64 * WGM * WGN * KG)) return too_large(M, N);
   hipLaunchKernelGGL((linear_dma_kernel<T, O, BM, BN, WGM, WGN, S, BKB, OCC, KG>), dim3(tiles_m * tiles_n), dim3(64 * WGM * WGN * KG), lds, st,
                      x, ldx, W, ldw, M, N, K, epi, tiles_m, tiles_n);
   QUAMBA_LAUNCH_CHECK();
@@ -621,6 +626,7 @@ int run_dma(const T *x, long long ldx, const T *W, long long ldw, int M, int N, 
 template <typename T, typename O, int TM, int TN>
 int run_any(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, hipStream_t st) {
   const int tiles_m = (M + 64 * TM - 1) / (64 * TM), tiles_n = (N + 64 * TN - 1) / (64 * TN);
+  if (!launchable((long long)tiles_m * tiles_n, 256)) return too_large(M, N);
   hipLaunchKernelGGL((linear_any_kernel<T, O, TM, TN>), dim3(tiles_m * tiles_n), dim3(256), 0, st, x, ldx, W, ldw, M, N, K, epi, tiles_m,
                      tiles_n);
   QUAMBA_LAUNCH_CHECK();
@@ -629,6 +635,7 @@ int run_any(const T *x, long long ldx, const T *W, long long ldw, int M, int N, 
 
 template <typename T, typename O, int MR>
 int run_vec(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, hipStream_t st) {
+  if (!launchable(K <= 1024 ? (N + 15) / 16 : (N + 3) / 4, 256)) return too_large(M, N);
   if (K <= 1024)
     hipLaunchKernelGGL((linear_vec_kernel<T, O, MR, 64>), dim3((N + 15) / 16), dim3(256), 0, st, x, ldx, W, ldw, M, N, K, epi);
   else
@@ -660,8 +667,7 @@ LinearPlan plan_linear(int M, int N, int K, bool wide_x, bool wide_w, size_t ws_
 template <typename T, typename O>
 int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int N, int K, const LinearEpi &epi, void *ws, size_t ws_bytes,
                hipStream_t st) {
-  if (((M + 31LL) / 32) * ((N + 31LL) / 32) > INT_MAX)
-    return fail(QUAMBA_EUNSUPPORTED, "linear: %d x %d outputs are more than one launch takes", M, N);
+  if (((M + 31LL) / 32) * ((N + 31LL) / 32) > INT_MAX) return too_large(M, N);
   if (M > 1 << 30 || N > 1 << 30 || K > 1 << 30) return fail(QUAMBA_EUNSUPPORTED, "linear: M=%d N=%d K=%d (at most 2^30 each)", M, N, K);
   const LinearPlan p = plan_linear(M, N, K, rows_wide(x, ldx, K), rows_wide(W, ldw, K), ws_bytes);
   if (p.copy_x || p.copy_w) {
@@ -669,7 +675,9 @@ int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int 
     const int per_row = (int)align_up(K, kCopyUnit) / 8;
     const RowCopy<T> cx{x, ldx, p.copy_x ? (long long)M * per_row : 0, reinterpret_cast<T *>(at)};
     const RowCopy<T> cw{W, ldw, p.copy_w ? (long long)N * per_row : 0, reinterpret_cast<T *>(at + (p.copy_x ? aligned_bytes(M, K) : 0))};
-    hipLaunchKernelGGL(align_rows_kernel<T>, dim3((unsigned)((cx.chunks + cw.chunks + 255) / 256)), dim3(256), 0, st, cx, cw, per_row, K);
+    const long long wgs = (cx.chunks + cw.chunks + 255) / 256;
+    hipLaunchKernelGGL(align_rows_kernel<T>, dim3((unsigned)(wgs < kCopyGrid ? wgs : kCopyGrid), (unsigned)((wgs + kCopyGrid - 1) / kCopyGrid)),
+                       dim3(256), 0, st, cx, cw, per_row, K);
     QUAMBA_LAUNCH_CHECK();
     if (p.copy_x) x = cx.to, ldx = per_row * 8LL;
     if (p.copy_w) W = cw.to, ldw = per_row * 8LL;
@@ -679,6 +687,7 @@ int run_linear(const T *x, long long ldx, const T *W, long long ldw, int M, int 
     case 0: return run_any<T, O, 1, 1>(x, ldx, W, ldw, M, N, K, epi, st);
     case 1: return run_any<T, O, 2, 2>(x, ldx, W, ldw, M, N, K, epi, st);
     case 2:
+      if (!launchable((N + 15) / 16, 512)) return too_large(M, N);
       hipLaunchKernelGGL((linear_rows_kernel<T, O>), dim3((N + 15) / 16), dim3(512), 0, st, x, ldx, W, ldw, M, N, K, epi);
       QUAMBA_LAUNCH_CHECK();
       return QUAMBA_OK;

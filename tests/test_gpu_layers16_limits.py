@@ -166,3 +166,17 @@ def test_linattn_with_any_workspace(shape):
         ld = c.rows.stride(1)
         Q.quamba_linattn_prefill(Q.TYPE_BF16, q, ld, k, ld, v, ld, c.g, c.Hv, None, *shape, c.scale, c.out, c.out.stride(1), c.state, ws)
         c.check(want)
+
+
+def test_linear_copies_of_more_than_four_gigabytes():
+    """4200 rows of 524225 elements, none of which starts on 16 bytes: more workgroups of the copy than one dimension of its launch has."""
+    M, N, K = 4200, 40, (1 << 19) - 63
+    at = torch.tensor([0, 7, 8, 1000, 300001, K - 2, K - 1], device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    x, W = (torch.zeros((rows, K), dtype=torch.bfloat16, device=DEV) for rows in (M, N))
+    a, b = (torch.randint(-8, 9, (rows, len(at)), generator=g, device=DEV) for rows in (M, N))
+    x[:, at], W[:, at] = a.bfloat16(), b.bfloat16()
+    ws = torch.full((Q.quamba_linear_workspace_bytes(M, N, K),), 255, dtype=torch.uint8, device=DEV)
+    out = torch.full((M, N), float("nan"), device=DEV)
+    Q.quamba_linear(Q.TYPE_BF16, x, K, W, K, None, None, 0, M, N, K, Q.ACT_NONE, Q.TYPE_F32, out, N, ws)
+    assert np.array_equal(out.cpu().numpy(), a.cpu().numpy().astype(np.float32) @ b.cpu().numpy().astype(np.float32).T)

@@ -3,6 +3,7 @@ import pytest
 
 import paper_2410_13229_amd as Q
 
+P = 1 << 20  # a made-up, aligned address: never touched
 COPY_X, COPY_W = 16, 32
 LONG = 1 << 21  # elements of a row from which a tile's rows may not lie within 2^31 bytes
 
@@ -45,3 +46,18 @@ def test_linattn_cuts_a_prompt_into_as_many_segments_as_the_workspace_holds():
         assert segments == 1 or segments * 80 * (128 * 64 * 4 + 8) <= room
         last = segments
     assert Q.quamba_debug_linattn_blocks(1, 2048, 80, 128, 64, 0) == 32
+
+
+@pytest.mark.parametrize("M, N, K", [(1, 1 << 26, 2048), (2, 1 << 28, 8), (16, 1 << 27, 7), (4, 1 << 26, 2049)])
+def test_linear_refuses_more_columns_than_a_launch_takes(M, N, K):
+    """A launch counts its threads in 32 bits."""
+    with pytest.raises(Q.QuambaError) as e:
+        Q.quamba_linear(Q.TYPE_F16, P, K, P, K, None, None, 0, M, N, K, Q.ACT_NONE, Q.TYPE_F16, P, N, None)
+    assert e.value.code == -2 and "more than one launch" in str(e.value)
+
+
+@pytest.mark.parametrize("Bt, Hv, dv", [(65535, 257, 1), (1 << 14, 1 << 9, 129), (1 << 12, 1 << 12, 1)])
+def test_linattn_prefill_refuses_more_workgroups_than_a_launch_takes(Bt, Hv, dv):
+    with pytest.raises(Q.QuambaError) as e:
+        Q.quamba_linattn_prefill(Q.TYPE_F16, P, Hv, P, Hv, P, Hv * dv, None, 0, None, Bt, 1, Hv, Hv, 1, dv, 1.0, P, Hv * dv, None, None)
+    assert e.value.code == -2 and "more than one launch" in str(e.value)
