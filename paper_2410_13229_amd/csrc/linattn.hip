@@ -3,6 +3,7 @@
 #include <atomic>
 #include <cfloat>
 #include <climits>
+#include <cstddef>
 #include <type_traits>
 
 #include "common.h"
@@ -133,7 +134,7 @@ struct SegArgs {
   float2 *decays;        // [Bt Hv][segments]: a segment's whole decay, fp32 and what that rounding left over
 };
 
-struct GTable {  // of a block's 64 tokens
+struct alignas(16) GTable {  // of a block's 64 tokens; read four floats at a time
   float d[kBlock];     // G_t to the nearest multiple of 2^-10, less 200 for each reset up to the token
   float up[kBlock];    // scale exp2 of what the rounding left over,
   float down[kBlock];  // and exp2 of its opposite: scale exp2(G_t - G_s) = exp2(d_t - d_s) up_t down_s
@@ -144,6 +145,8 @@ struct GTable {  // of a block's 64 tokens
   float dec;           // the factor of the state
   int resets;
 };
+static_assert(sizeof(GTable) % 16 == 0 && offsetof(GTable, d) % 16 == 0 && offsetof(GTable, down) % 16 == 0 && offsetof(GTable, w) % 16 == 0,
+              "both tables' rows start on 16 bytes");
 
 // 2^x for x <= 0, to 7e-12
 __device__ __forceinline__ double exp2_neg(double x) {
