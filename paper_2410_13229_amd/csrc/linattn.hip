@@ -337,14 +337,18 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 // 16 bytes a lane from base + off (lane) + soff (wave) to consecutive LDS from `to` on, zeros where off is negative.  Written
 // out, because the compiler takes every LDS read for one of what such a load is still bringing and waits for the load first (three
 // times a block; 2 x 4000, 32 heads of 64 x 64: 72 -> 67 us).  What it would know is kept by hand: nothing reads a tile before
-// the barrier that waits for its loads, and the scalar operands may come straight from a vector instruction, hence the five wait states (and m0
-// is nobody else's: of what the compiler writes here, only its own direct-to-LDS loads would use it).
+// the barrier that waits for its loads, and the scalar operands may come straight from a vector instruction, hence the five wait states.
+// m0 is declared; the warning that goes with it says that the compiler reserves m0 and would not save it, and it keeps nothing there.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void tile_load(const void *base, int off, int soff, const char *to) {
   const unsigned long long b = reinterpret_cast<unsigned long long>(base);
   const u4 rsrc = {(unsigned)b, (unsigned)(b >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
   const unsigned lds = (unsigned)reinterpret_cast<unsigned long long>((const __attribute__((address_space(3))) char *)to);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(off), "s"(rsrc), "s"(soff));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(off), "s"(rsrc), "s"(soff)
+               : "m0");
 }
+#pragma clang diagnostic pop
 
 // Eight elements of a row of K from element k on, zeros behind K and where the row is off, in two steps: what is in flight is 16
 // bytes that end with the row at the latest, and they are moved into place when they are used.  With the last elements loaded one

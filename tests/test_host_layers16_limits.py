@@ -1,4 +1,7 @@
 """What the 16-bit layers choose and refuse near the limits of their sizes: decided on the host, so no GPU is needed."""
+import os
+import re
+
 import pytest
 
 import paper_2410_13229_amd as Q
@@ -61,3 +64,11 @@ def test_linattn_prefill_refuses_more_workgroups_than_a_launch_takes(Bt, Hv, dv)
     with pytest.raises(Q.QuambaError) as e:
         Q.quamba_linattn_prefill(Q.TYPE_F16, P, Hv, P, Hv, P, Hv * dv, None, 0, None, Bt, 1, Hv, Hv, 1, dv, 1.0, P, Hv * dv, None, None)
     assert e.value.code == -2 and "more than one launch" in str(e.value)
+
+
+def test_the_direct_to_lds_load_declares_the_register_it_writes():
+    """m0 is written inside the statement: a compiler that is not told could take an older value of its own for still there."""
+    source = open(os.path.join(os.path.dirname(Q.__file__), "csrc", "linattn.hip")).read()
+    statements = re.findall(r"asm volatile\(([^;]*?)\);", source, re.S)
+    writes = [s for s in statements if "s_mov_b32 m0" in s]
+    assert writes and all(s.rstrip().endswith('"m0"') for s in writes)
