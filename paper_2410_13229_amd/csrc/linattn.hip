@@ -148,17 +148,23 @@ struct alignas(16) GTable {  // of a block's 64 tokens; read four floats at a ti
 static_assert(sizeof(GTable) % 16 == 0 && offsetof(GTable, d) % 16 == 0 && offsetof(GTable, down) % 16 == 0 && offsetof(GTable, w) % 16 == 0,
               "both tables' rows start on 16 bytes");
 
+// A constant in scalar registers, made where it is used: as vector registers those of the polynomial below are kept through the loop,
+// and where there are none left for them, in scratch memory.
+__device__ __forceinline__ double literal(double c) {
+  asm volatile("" : "+s"(c));
+  return c;
+}
 // 2^x for x <= 0, to 7e-12
 __device__ __forceinline__ double exp2_neg(double x) {
   if (!(x > -200.0)) return x == x ? 0.0 : x;
-  const double n = __builtin_rint(x), f = (x - n) * 0.69314718055994530942;
-  double p = 1.0 / 362880.0;
-  p = __builtin_fma(p, f, 1.0 / 40320.0);
-  p = __builtin_fma(p, f, 1.0 / 5040.0);
-  p = __builtin_fma(p, f, 1.0 / 720.0);
-  p = __builtin_fma(p, f, 1.0 / 120.0);
-  p = __builtin_fma(p, f, 1.0 / 24.0);
-  p = __builtin_fma(p, f, 1.0 / 6.0);
+  const double n = __builtin_rint(x), f = (x - n) * literal(0.69314718055994530942);
+  double p = literal(1.0 / 362880.0);
+  p = __builtin_fma(p, f, literal(1.0 / 40320.0));
+  p = __builtin_fma(p, f, literal(1.0 / 5040.0));
+  p = __builtin_fma(p, f, literal(1.0 / 720.0));
+  p = __builtin_fma(p, f, literal(1.0 / 120.0));
+  p = __builtin_fma(p, f, literal(1.0 / 24.0));
+  p = __builtin_fma(p, f, literal(1.0 / 6.0));
   p = __builtin_fma(p, f, 0.5);
   p = __builtin_fma(p, f, 1.0);
   p = __builtin_fma(p, f, 1.0);

@@ -5,6 +5,7 @@ import re
 import pytest
 
 import paper_2410_13229_amd as Q
+from paper_2410_13229_amd import build
 
 P = 1 << 20  # a made-up, aligned address: never touched
 COPY_X, COPY_W = 16, 32
@@ -72,3 +73,20 @@ def test_the_direct_to_lds_load_declares_the_register_it_writes():
     statements = re.findall(r"asm volatile\(([^;]*?)\);", source, re.S)
     writes = [s for s in statements if "s_mov_b32 m0" in s]
     assert writes and all(s.rstrip().endswith('"m0"') for s in writes)
+
+
+def _remarks(name, scratch, vgprs, sgprs):
+    return "".join("x.hip:1:1: remark: %s [-Rpass-analysis=kernel-resource-usage]\n" % r for r in (
+        "Function Name: " + name, "    ScratchSize [bytes/lane]: %d" % scratch, "    SGPRs Spill: %d" % sgprs, "    VGPRs Spill: %d" % vgprs))
+
+
+@pytest.mark.parametrize("name, scratch, vgprs, sgprs, refused", [
+    ("_Z21linattn_blocks_kernelIDF16_E", 52, 16, 90, True), ("_Z21linattn_blocks_kernelIDF16_E", 0, 2, 0, True),
+    ("_Z21linattn_blocks_kernelIDF16_E", 0, 0, 90, False), ("_Z17linear_dma_kernelIDF16_E", 0, 0, 1, True),
+    ("_Z17linear_dma_kernelIDF16_E", 0, 0, 0, False), ("_Z19linattn_step_kernelIDF16_E", 8, 2, 70, False)])
+def test_the_build_refuses_scratch_memory_where_loads_are_counted(name, scratch, vgprs, sgprs, refused):
+    if refused:
+        with pytest.raises(RuntimeError, match="spills"):
+            build._check_spills(_remarks(name, scratch, vgprs, sgprs))
+    else:
+        build._check_spills(_remarks(name, scratch, vgprs, sgprs))
