@@ -392,17 +392,17 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, OCC) void linear_dma_kernel(co
       mma(fx, fw);
     }
   } else {
-    // iteration k: slice k has landed (at most the loads issued after it are outstanding), everyone is done with slice k - 1,
-    // whose stage slice k + S - 1 takes
+    // iteration k: slice k has landed (at most the loads issued after it are outstanding), everyone is done with slice k - 1 (its LDS
+    // reads are waited for here, not only by the products that use them), whose stage slice k + S - 1 takes
 #pragma unroll
     for (int s = 0; s < S - 1; ++s)
       if (s < nk) issue(s, s);
     int stage = 0;
     for (int kt = 0; kt < nk; ++kt) {
       if (kt + S - 2 < nk)
-        __builtin_amdgcn_s_waitcnt(QUAMBA_VMCNT((S - 2) * NI));
+        __builtin_amdgcn_s_waitcnt(QUAMBA_VMCNT_LGKM0((S - 2) * NI));
       else
-        __builtin_amdgcn_s_waitcnt(QUAMBA_VMCNT(0));  // tail: fewer slices were issued
+        __builtin_amdgcn_s_waitcnt(QUAMBA_VMCNT_LGKM0(0));  // tail: fewer slices were issued
       __builtin_amdgcn_s_barrier();
       if (kt + S - 1 < nk) issue(stage == 0 ? S - 1 : stage - 1, kt + S - 1);
 #pragma unroll
