@@ -293,11 +293,11 @@ __device__ __forceinline__ Half<__bf16>::v8 weight_operand(const char *p, int t,
   return both(*reinterpret_cast<const v4 *>(p + weight_at(t, chunk) + off), *reinterpret_cast<const v4 *>(p + weight_at(t, chunk + 2) + off));
 }
 
-// The power of two (its exponent) that brings m to 2^12 .. 2^13, the top of fp16's range, limited so that it stays an ordinary
-// fp32 number
+// The power of two (its exponent) that brings m to 2^12 .. 2^13, the top of fp16's range, whatever fp32 number m is (at least -116); at
+// most 2^100, so that its inverse times a decay stays an ordinary number.
 __device__ __forceinline__ int top_exponent(float m) {
   const int e = 127 + 12 - (int)((__float_as_uint(m) >> 23) & 0xff);
-  return min(max(e, -100), 100);
+  return min(e, 100);
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(127 + e) << 23); }
 // Largest over the four lane groups (the same column)

@@ -180,3 +180,19 @@ def test_linear_copies_of_more_than_four_gigabytes():
     out = torch.full((M, N), float("nan"), device=DEV)
     Q.quamba_linear(Q.TYPE_BF16, x, K, W, K, None, None, 0, M, N, K, Q.ACT_NONE, Q.TYPE_F32, out, N, ws)
     assert np.array_equal(out.cpu().numpy(), a.cpu().numpy().astype(np.float32) @ b.cpu().numpy().astype(np.float32).T)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("power", [-80, 100, 112, 116, 120])
+@pytest.mark.parametrize("shape", [(1, 130, 1, 2, 64, 64), (1, 70, 1, 1, 128, 100), (2, 66, 1, 2, 33, 19)])
+def test_linattn_states_of_any_size(shape, power, dt):
+    """The state is fp32, and 2^122 is one of its values also beside fp16 operands."""
+    c = Call(*shape, dt)
+    c.state *= 2.0 ** power
+    c.scale = 2.0 ** -power
+    q, k, v = c.parts()
+    if power < 0:
+        k.zero_()  # their products would be all there is
+    want = c.want()
+    c.prefill()
+    c.check(want)
