@@ -118,8 +118,11 @@ int run_step(const LinAttnArgs &a, hipStream_t st) {
 // fp32 values go through the 16-bit matrix units in pieces, each the rounding of what the ones before left over:
 //   S in front of q: two pieces (16 bits), the block's weights two bf16 pieces, the weighted v of the state's update three bf16
 //   pieces (24 bits) or two fp16 ones (22).  bf16 pieces have fp32's range.  fp16 operands (k, q) need fp16 partners, so a
-//   column of S or of the weighted v is first brought to the top of fp16's range by a power of two; v itself splits into two
-//   bf16 pieces exactly.
+//   column of S or of the weighted v is first brought to the top of fp16's range by a power of two, and what is below 2^-37 of its
+//   largest element is lost (S in front of q has 22 bits there); v itself splits into two bf16 pieces exactly, whose lower one meets the
+//   weights' upper one only (2^-18 of a product is left out).
+// These are fewer bits than fp32's in front of a product only: states, sums and their joins are fp32.  16 bits are 2^8 (bf16) or 2^5 (fp16)
+// times finer than the outputs they end in; the update's have to last, hence 22 and 24.  A third piece of S costs a fifth more products.
 // A decay of -infinity (or below fp32's range) is a reset: it adds nothing to G, but weights across it are 0.
 //
 // The exponents G_t - G_s are differences of sums that grow by up to 126 a token, and what fp32 rounds off a sum of 2000 is 2^-14 of

@@ -196,3 +196,36 @@ def test_linattn_states_of_any_size(shape, power, dt):
     want = c.want()
     c.prefill()
     c.check(want)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("what", ["state", "v"])
+def test_linattn_columns_of_a_wide_range(what, dt):
+    """Elements of a column that differ by 2^40 and keys that take them apart.  fp16 pieces are relative to the column's largest
+    element: 22 bits of those near it, and of what is smaller all that is above 2^-37 of it; bf16 pieces keep theirs anywhere."""
+    B, L, dk, dv = 1, 64, 64, 64
+    c = Call(B, L, 1, 1, dk, dv, dt, decay="none")
+    q, k, v = c.parts()
+    eye = torch.eye(64, device=DEV)
+    small = torch.exp2(-torch.arange(64, device=DEV).remainder(41).float())
+    q.copy_(eye[None].expand_as(q))  # token t asks for row t
+    if what == "state":
+        k.zero_(), v.zero_()
+        c.state = (1 + torch.rand((B, 1, dk, dv), device=DEV, generator=torch.Generator(device=DEV).manual_seed(3))) * small[None, None, :, None] * 2.0 ** 20
+        most = 2.0 ** 21
+    else:
+        k.copy_(eye[None].expand_as(k))  # token t writes row t
+        v.copy_((v.float() * (small * 2.0 ** 12 + 2.0 ** -14)[None, :, None]).to(dt))
+        c.state.zero_()
+        most = float(v.abs().max())
+    c.scale = 2.0 ** -6  # outputs within fp16
+    out, S, out_size, size = c.want()
+    c.prefill()
+    lost = 2.0 ** -37 * most if dt == torch.float16 else 0.0
+    e = torch.finfo(dt)
+    t_out = ((64 + dk + 16) * U + 2.0 ** -16) * out_size + c.scale * lost
+    t_out = t_out + e.eps / 2 * (np.abs(out) + t_out) + e.smallest_normal * e.eps
+    off = np.abs(_f64(c.out).reshape(out.shape) - out) / t_out
+    assert off.max() <= 1, "output off by %.2f of what it may be" % off.max()
+    off = np.abs(_f64(c.state) - S) / ((16 * U + 2.0 ** -21) * size + lost + 1e-37)
+    assert off.max() <= 1, "state off by %.2f of what it may be" % off.max()
