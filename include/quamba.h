@@ -584,7 +584,10 @@ int quamba_model_generate(const quamba_model *model, const int32_t *first_tokens
  *   between calls of different M (another order of the sums).
  *   ws (256-byte aligned, may be NULL): quamba_linear_workspace_bytes bytes make room for copies of x and W with rows on 16
  *   bytes, which a product of more than 16 rows is computed from if theirs do not start there (pointer, stride and K); without
- *   them such a product takes about twice the time.  Not used otherwise.  M = 0 is allowed and does nothing. */
+ *   them such a product takes about twice the time.  The query knows no strides: a program whose rows of x and W start on 16 bytes
+ *   needs no workspace, one with copies of one of them only align_up(rows * align_up(K, 64) * 2, 256) bytes for it.  Rows of 2^21
+ *   elements and more are never copied.  M, N, K up to 2^30; outputs that one launch does not take (2^26 columns of one or two
+ *   rows) are refused.  M = 0 is allowed and does nothing. */
 #define QUAMBA_TYPE_F16 1
 #define QUAMBA_TYPE_BF16 2
 #define QUAMBA_TYPE_F32 3
@@ -608,13 +611,18 @@ int quamba_linear(int type, const void *x, int ldx, const void *W, int ldw, cons
  *   pass NULL (start from zero, keep nothing).
  * quamba_linattn_prefill runs prompts: lens int32 [Bt] (device, may be NULL = L each) gives each sequence's length, clamped to
  * [0, L]; tokens behind it are not read, their output rows are left as they were, and an empty sequence keeps its state.  The sums are
- * taken block by block: the result is that of the recurrence up to the rounding of fp32 sums (block weights carry 16 bits or more,
- * the state's update 22 or more).  ws (256-byte aligned, may be NULL): with quamba_linattn_workspace_bytes a sequence is cut into as
- * many segments as pay; with less, into fewer (one needs no room), which may take twice the time and adds the sums in another order.  A
- * larger batch or prompt may need less, so a program with several shapes takes the largest of their queries.
+ * taken block by block, 64 tokens at a time: the result is that of the recurrence up to the rounding of fp32 sums, but in front of the
+ * matrix units the block's weights and the state that meets q carry 16 bits or more, the state's update 22 or more; with fp16
+ * operands the state's and the update's bits are relative to the largest element of their column (of dk rows or 64 tokens), and what is
+ * below 2^-37 of it is lost.  What decays by more than 2^-126 within a block counts as 0.  q k, k v and q S have to stay within fp32.
+ * ws (256-byte aligned, may be NULL): with quamba_linattn_workspace_bytes a sequence is cut into as many segments as pay; with less, into
+ * fewer (one needs no room), which takes longer (1 x 2048, 80 heads of 128 x 64: 58 and 115 us; 1 x 16384, one head of 64 x 64: 33
+ * and 617) and adds the sums in another order.  A larger batch or prompt may need less, so a program with several shapes takes the largest of
+ * their queries.
  * Infinities and NaN stay out of everything before their token: one in v makes its column of outputs and state NaN or infinite
- * from its token on, one in k or g its head's; a reset does not clear a state that holds one.
+ * from its token on, one in g its head's, one in k those of the heads that read it; a reset does not clear a state that holds one.
  * quamba_linattn_step is one token of every sequence (L = 1, state required), strides between sequences.
+ * Bt and Hv up to 65535, L up to 2^30; more workgroups than one launch takes (2^24) are refused.
  * out must not overlap an input, state no other buffer.  Bt = 0 or L = 0 does nothing. */
 size_t quamba_linattn_workspace_bytes(int Bt, int L, int Hk, int Hv, int dk, int dv);
 int quamba_linattn_prefill(int type, const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, const float *log_decay,

@@ -954,6 +954,8 @@ size_t prefill_workspace(const AttnPlan &p, int Bt, int Hv, int dk, int dv) {
 // to 65536 tokens, dk 32 to 256) the choice is within 10 % of the best of up to 16 that were timed: 1 x 2048, 80 heads of 128 x 64,
 // 6 blocks a segment 58 us, 4 66, 8 67, all in one 115; 8 x 256, 16 heads of 64 x 64, all in one 15.5, 2 blocks 21.5, single ones
 // 23.7; 1 x 16384, one head of 64 x 64, 3 blocks 33, single ones 44, all in one 617.
+// The constants are those of rows on 16 bytes: the workspace query, which has to plan alike, does not know the strides.  Rows off 16
+// bytes run one column tile a wave also where dv > 64 (run_prefill), up to twice the workgroups that are counted here.
 // What `room` does not hold is left out; one segment needs none, so a workspace that another shape asked for serves too.
 AttnPlan plan_prefill(int Bt, int L, int Hv, int dk, int dv, size_t room = SIZE_MAX) {
   AttnPlan p{2, 1, 1, 1};

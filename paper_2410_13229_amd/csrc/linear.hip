@@ -26,8 +26,9 @@ struct LinearEpi {
 };
 
 // 0.5 erfc(z / sqrt 2) for z >= 0: with y = z / sqrt 2 and t = 1 / (1 + 0.4 y), erfc(y) = exp(-y^2) t p(t), p of degree 8
-// fitted to erfc(y) exp(y^2) / t over 0 < t <= 1 by least squares whose weights were moved towards equal errors (1.3e-7 of the
-// value).  A relative error, so the far tail of GELU is as good as its middle; a third of the instructions of erfcf.
+// fitted to erfc(y) exp(y^2) / t over 0 < t <= 1 by least squares whose weights were moved towards equal errors (1.5e-7 of the
+// value).  A relative error; in fp32 the rounding of z^2 in the exponent adds to it, 2e-6 up to z = 6, 7e-6 at 12.  A third of the
+// instructions of erfcf.
 __device__ __forceinline__ float upper_tail(float z) {
   const float t = __builtin_amdgcn_rcpf(fmaf(0.4f * 0.70710678118654752440f, z, 1.f));
   float p = 0.02512870542705059f;
@@ -577,10 +578,22 @@ std::atomic<int> g_linear_variant{-1};
 //   0, 1 = any alignment, 64 x 64 and 128 x 128 tiles     2 = rows straight to the matrix unit (M <= 16)     10 = vector unit (M <= 4)
 //   direct-to-LDS tiles: 3 = 256 x 320, 4 = 256 x 256 (8 waves, ring of 2)   5 = 128 x 128 (ring of 2, two workgroups a CU)
 //   6 = 64 x 64 (ring of 3)   7 = 32 x 32, 4 K groups   8 = 64 x 64, 2 K groups   9 = 128 x 128, 2 K groups   11 = 32 x 32, 8 K groups
+// The aligned ones by how many of their tiles are resident at once on 256 CUs: 11, 8, 9 and 3, 4 one to a CU, 7, 6 and 5 two.  Up to
+// one round the smaller tile wins, past it the next.  us a call on both sides of each bound (bf16, calls of a captured graph):
+//   one or two rows, 10 against 7 and 11, W from memory: 1 x 10240 x 2560 12.6, 13.5 and 16.4, 2 x 2560 x 5120 10.8, 17.2 and 12.7; at three
+//   rows 18.7, 13.5 and 16.5, at 2 x 10240 x 2560 already 14.7, 13.5 and 16.6
+//   11 against 7, 64 rows: N = 2560 K = 5120 10.9 and 12.8, K = 2048 6.5 and 7.0, K = 1024 4.4 and 4.5; 288 tiles K = 5120 20.2 and 18.9
+//   7 against 8: 512 tiles (64 x 8192 x 2560) 11.4 and 12.0; 576 14.7 and 12.2
+//   8 against 6: 256 tiles (256 x 4096 x 2560) 12.3 and 15.0; 288 21.8 and 19.3
+//   6 against 9: 512 tiles (512 x 4096 x 2560) 21.2 and 24.5; 560 27.2 and 24.9, at K = 1280 15.4 and 16.1; 640 27.6 and 25.0
+//   9 against 5: 256 tiles (1024 x 4096 x 2560) 28.6 and 33.9; 288 48.7 and 35.4
+//   5 against 4: 512 tiles (2048 x 4096 x 2560) 44.1 and 60.2; 576 70.5 and 61.1
+//   3, 4 and 5 past that: 2048 x 10240 x 2560 90, 144 and 128; 4096 x 4096 x 4096 122, 109 and 130; 2560 x 8192 x 4096 232, 204 and 184
+// Rows off 16 bytes that are not copied: 10 against 2 at 1 x 2560 x 2561 6.2 and 8.0, at 4 x 10240 x 2561 23.4 and 19.9, at 4 x 2560 x 5121
+// 11.3 and 10.8; 0 against 1 at 240 tiles of 128 x 128 (2048 x 1920 x 2561) 62 and 68, at 288 98 and 69; copied, these take 38 and 45.
 constexpr int kLinearKinds = 12;
 
-int pick_kind(int M, int N, int K, bool wide) {
-  const int forced = g_linear_variant.load(std::memory_order_relaxed);
+int pick_kind(int M, int N, int K, bool wide, int forced) {
   if (forced >= 0 && forced < kLinearKinds && (forced != 2 || M <= 16) && (forced != 10 || M <= 4) && (forced < 3 || forced == 10 || wide))
     return forced;
   if (M <= 2 || (M <= 4 && !wide)) return 10;
@@ -593,7 +606,8 @@ int pick_kind(int M, int N, int K, bool wide) {
   if (t64 <= 560) return 6;
   if (t128 <= 256) return 9;
   if (t128 <= 512) return 5;
-  // rounds of 256 CUs times the area of a tile; the 128 x 128 ones run two to a CU at 0.9 of the others' rate
+  // rounds of 256 CUs times the area of a tile; the 128 x 128 ones run two to a CU at 0.9 of the others' rate (8192 x 4096 x 8192, whole
+  // rounds of both: 499 us and 428)
   auto rounds = [](long long t, long long n) { return (double)((t + n - 1) / n); };
   const double e3 = rounds(tiles(256, 320), 256) * (256.0 * 320.0), e4 = rounds(tiles(256, 256), 256) * (256.0 * 256.0);
   const double e5 = rounds(t128, 512) * (2.0 * 128.0 * 128.0) * 1.1;
@@ -650,8 +664,8 @@ constexpr int kLongRow = 1 << 21;
 bool rows_wide(const void *p, long long ld, int K) { return aligned(p, 16) && ld % 8 == 0 && K % 8 == 0 && ld < kLongRow; }
 constexpr int kCopyUnit = 64;  // elements a copied row is a multiple of: whole 128-byte lines
 size_t aligned_bytes(int rows, int K) { return align_up((size_t)rows * align_up(K, kCopyUnit) * 2, 256); }
-// More rows than the streaming kernels take: operands of any alignment are worth copying to 16-byte rows first, unless the copies
-// would again be too long for the kernels that want them.
+// More rows than the streaming kernels take: operands of any alignment are worth copying to 16-byte rows first (17 x 2560 x 2561 with the copy
+// 16 us, without 40; 16 rows without 9.6), unless the copies would again be too long for the kernels that want them.
 bool copies(int M, int K) { return M > 16 && align_up(K, kCopyUnit) < kLongRow; }
 
 struct LinearPlan {
@@ -659,9 +673,9 @@ struct LinearPlan {
   int kind;
 };
 LinearPlan plan_linear(int M, int N, int K, bool wide_x, bool wide_w, size_t ws_bytes) {
-  const bool copy = copies(M, K) && !(wide_x && wide_w) && (wide_x ? 0 : aligned_bytes(M, K)) + (wide_w ? 0 : aligned_bytes(N, K)) <= ws_bytes &&
-                    g_linear_variant.load(std::memory_order_relaxed) < 0;
-  return LinearPlan{copy && !wide_x, copy && !wide_w, pick_kind(M, N, copy ? (int)align_up(K, 8) : K, copy || (wide_x && wide_w))};
+  const int forced = g_linear_variant.load(std::memory_order_relaxed);
+  const bool copy = copies(M, K) && !(wide_x && wide_w) && (wide_x ? 0 : aligned_bytes(M, K)) + (wide_w ? 0 : aligned_bytes(N, K)) <= ws_bytes && forced < 0;
+  return LinearPlan{copy && !wide_x, copy && !wide_w, pick_kind(M, N, copy ? (int)align_up(K, 8) : K, copy || (wide_x && wide_w), forced)};
 }
 
 template <typename T, typename O>
