@@ -614,7 +614,7 @@ int quamba_linear(int type, const void *x, int ldx, const void *W, int ldw, cons
  * taken block by block, 64 tokens at a time: the result is that of the recurrence up to the rounding of fp32 sums, but in front of the
  * matrix units the block's weights and the state that meets q carry 16 bits or more, the state's update 22 or more; with fp16
  * operands the state's and the update's bits are relative to the largest element of their column (of dk rows or 64 tokens), and what is
- * below 2^-37 of it is lost.  What decays by more than 2^-126 within a block counts as 0.  q k, k v and q S have to stay within fp32.
+ * below 2^-37 of it is lost.  What decays by more than 2^-126 may count as 0.  q k, k v and q S have to stay within fp32.
  * ws (256-byte aligned, may be NULL): with quamba_linattn_workspace_bytes a sequence is cut into as many segments as pay; with less, into
  * fewer (one needs no room), which takes longer (1 x 2048, 80 heads of 128 x 64: 58 and 115 us; 1 x 16384, one head of 64 x 64: 33
  * and 617) and adds the sums in another order.  A larger batch or prompt may need less, so a program with several shapes takes the largest of
