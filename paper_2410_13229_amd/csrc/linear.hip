@@ -579,7 +579,8 @@ std::atomic<int> g_linear_variant{-1};
 //   direct-to-LDS tiles: 3 = 256 x 320, 4 = 256 x 256 (8 waves, ring of 2)   5 = 128 x 128 (ring of 2, two workgroups a CU)
 //   6 = 64 x 64 (ring of 3)   7 = 32 x 32, 4 K groups   8 = 64 x 64, 2 K groups   9 = 128 x 128, 2 K groups   11 = 32 x 32, 8 K groups
 // The aligned ones by how many of their tiles are resident at once on 256 CUs: 11, 8, 9 and 3, 4 one to a CU, 7, 6 and 5 two.  Up to
-// one round the smaller tile wins, past it the next.  us a call on both sides of each bound (bf16, calls of a captured graph):
+// one round the smaller tile wins, past it the next.  us a call on both sides of each bound (M x N x K, bf16, calls of
+// a captured graph):
 //   one or two rows, 10 against 7 and 11, W from memory: 1 x 10240 x 2560 12.6, 13.5 and 16.4, 2 x 2560 x 5120 10.8, 17.2 and 12.7; at three
 //   rows 18.7, 13.5 and 16.5, at 2 x 10240 x 2560 already 14.7, 13.5 and 16.6
 //   11 against 7, 64 rows: N = 2560 K = 5120 10.9 and 12.8, K = 2048 6.5 and 7.0, K = 1024 4.4 and 4.5; 288 tiles K = 5120 20.2 and 18.9

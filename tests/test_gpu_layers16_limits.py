@@ -28,8 +28,8 @@ def test_linear_rows_of_more_than_two_million_elements_with_a_workspace():
 
 
 def _closely(c, want):
-    """Call.check's bounds without a term for the decays: their sums keep 33 bits or more in front of the binary point's 2^-10, so a weight
-    is off by its exponential's unit and two roundings, which the 16 units of 2^-23 hold."""
+    """Call.check's bounds without a term for the decays: a weight's exponent is an exact difference and a factor, off by the units of
+    its exponentials and products, which the 16 units of 2^-23 hold."""
     out, S, out_size, size = want
     e = torch.finfo(c.dt)
     t_out = ((c.L + c.dk + 64 + 16) * U + 2.0 ** -16) * out_size
